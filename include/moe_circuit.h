@@ -54,6 +54,16 @@ typedef int moe_status;
 #define MOE_W_FP8_E4M3_B128   1   /* OCP FP8 E4M3 codes (S.1111.111 = NaN, no infinities) + one float
                                      scale per 128 x 128 block                                   */
 
+/* element types of the residual stream and of router logits */
+#define MOE_T_BF16                0
+#define MOE_T_F32                 1
+
+/* scores and flags of moe_router_topk */
+#define MOE_ROUTER_SOFTMAX        0
+#define MOE_ROUTER_SIGMOID        1
+#define MOE_ROUTER_RENORMALISE    1   /* the weights of a token's chosen experts are divided by their sum */
+#define MOE_ROUTER_MAX_TOPK       32
+
 /* ---------------------------------------------------------------------------------------------
  * moe_route_histogram -- Section 2.1 (dispatch) / Section 3 (the all-to-all communication
  * matrix between ranks).  For each of L independent layers:
@@ -311,6 +321,104 @@ moe_status moe_expert_ffn_backward_sliced(const void* x, const void* dy, const i
  * ------------------------------------------------------------------------------------------- */
 moe_status moe_combine_topk_sum(const void* y, const int32_t* row_of, const float* gate, int T, int topk, int d,
                                 int R, void* out, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * moe_combine_topk_sum_backward -- gradients of moe_combine_topk_sum (Section 2.1: in training the exchange is repeated
+ * for the gradients; d_y is what the experts' backward pass takes as dy, d_gate what the router's takes):
+ *     d_y[r]       = sum of gate[t][j] * d_out[t] over all (t, j) with row_of[t][j] == r   (zeros where there is none)
+ *     d_gate[t][j] = sum over the columns of d_out[t] * y[row_of[t][j]]                    (0 for a dropped assignment)
+ * Products and sums in fp32, d_y rounded to bf16 once.  A row that several assignments name gets their sum, added in the order of
+ * the assignments (t, j); such rows are found by going through row_of once each, so they are meant to be few.
+ *   d_out    in   bf16 [T][d]          y  in  bf16 [R][d]
+ *   row_of, gate  as in the forward call; without gate there is no d_gate (NULL)
+ *   d_y      out  bf16 [R][d], every row written          d_gate  out  float [T][topk]
+ *   workspace     moe_combine_backward_workspace_bytes(R) bytes
+ * Limits: d % 8 == 0, d <= 16384, T * topk < 2^31; d_out, y, d_y and the workspace 16-byte aligned.  HBM bound: (1 + 2 topk) * 2 * d
+ * bytes per token.
+ * ------------------------------------------------------------------------------------------- */
+size_t     moe_combine_backward_workspace_bytes(int R);
+moe_status moe_combine_topk_sum_backward(const void* d_out, const void* y, const int32_t* row_of, const float* gate, int T, int topk, int d, int R,
+                                         void* d_y, float* d_gate, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * moe_router_topk -- Section 2.1: the router sends each token to its topk experts.  From the logits of T tokens over E experts, per token:
+ *     ids   = the topk experts with the largest logits, in falling order; of equal logits the lower index first
+ *     gates = scale * score of these experts; score = softmax over all E logits or the sigmoid of the logit; with
+ *             MOE_ROUTER_RENORMALISE divided by the sum of the chosen experts' scores
+ * A logit of -infinity (or NaN) is masked: its expert has a score of zero and is not chosen; a slot for which no expert is left gets
+ * id -1, which moe_route_histogram ignores, and the weight 0.  Logits of +infinity share the softmax evenly.
+ *   logits   in   [T][E], bf16 or float (logits_type: MOE_T_BF16 / MOE_T_F32)
+ *   ids      out  int32 [T][topk]  (what moe_route_histogram and moe_slice_table take as ids of a source rank)
+ *   gates    out  float [T][topk]  (what moe_combine_topk_sum takes as gate)
+ * moe_router_topk_backward -- the gradient of the logits from that of the gates, through the scores of the chosen experts (the choice itself has no
+ * gradient): d_logits [T][E] in the type of the logits, every entry written; masked logits get 0.  ids as the forward call
+ * returned them; slots outside [0, E) or of masked experts contribute nothing, an expert that is named twice gets the sum.
+ * Scores, sums and gradients in fp32.
+ * Limits: 1 <= topk <= min(E, MOE_ROUTER_MAX_TOPK), E <= MOE_MAX_EXPERTS, scale finite; pointers aligned to their elements.
+ * ------------------------------------------------------------------------------------------- */
+moe_status moe_router_topk(const void* logits, int logits_type, int T, int E, int topk, int score, int flags, float scale,
+                           int32_t* ids, float* gates, void* hip_stream);
+moe_status moe_router_topk_backward(const float* d_gates, const void* logits, int logits_type, const int32_t* ids, int T, int E, int topk,
+                                    int score, int flags, float scale, void* d_logits, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * moe_block_norm, moe_block_join -- Section 2.1: a MoE block stands between residual connections.  The norms before and after
+ * it, its token gate and the residual scale, each row read and written once:
+ *     norm:  out[t]  = x[t] / rms(x[t]) * weight                       rms(v) = sqrt(mean(v^2) + eps)
+ *     join:  u       = z[t] / rms(z[t]) * post_weight    (without post_weight: u = z[t])
+ *            out[t]  = scale * stream[t] + gate[t] * u   (without gate: gate = 1)
+ *            next[t] = out[t] / rms(out[t]) * next_weight              (the input of the next block; without next_weight: not made)
+ * Arithmetic in fp32, next from out before out is rounded; a row whose sum of squares passes the range of fp32 counts as
+ * infinitely long (normalised to zeros).
+ *   x, stream, out (of join)  [T][d], bf16 or float (stream_type: MOE_T_BF16 / MOE_T_F32): the residual stream
+ *   z, next, out (of norm)    bf16 [T][d]            weights  float [d]            gate  float [T]
+ *   out may be the stream itself, and next may be z (the same pointer): a row is read before it is written.
+ * moe_block_norm_backward -- from d_out (bf16 [T][d], the gradient of norm's out):
+ *     d_x = d_stream + the gradient of x through the norm     (d_stream: the gradient that arrived along the stream, NULL = none)
+ *     d_weight = sum over the tokens
+ * moe_block_join_backward -- from d_out (gradient of out along the stream, stream_type; NULL = none) and d_next (bf16; with next_weight only),
+ * with out as the forward call returned it:
+ *     d_stream (stream_type), d_z (bf16), and for each of post_weight, gate and next_weight that is given its gradient
+ *     (float; NULL where the input is NULL).  d_stream may be d_out and d_z may be d_next (the same pointer).
+ * Sums over columns and tokens in fp32; the tokens are added in an order that depends on T, d and the number of compute units alone.
+ *   workspace  moe_block_backward_workspace_bytes(T, d) bytes (sums over groups of tokens)
+ * Limits: d % 8 == 0, d <= 16384, 0 < eps < infinity, scale finite; every pointer but gate and d_gate 16-byte aligned.  HBM bound.
+ * ------------------------------------------------------------------------------------------- */
+size_t     moe_block_backward_workspace_bytes(int T, int d);
+moe_status moe_block_norm(const void* x, int stream_type, const float* weight, float eps, int T, int d, void* out, void* hip_stream);
+moe_status moe_block_norm_backward(const void* d_out, const void* x, int stream_type, const float* weight, const void* d_stream, float eps,
+                                   int T, int d, void* d_x, float* d_weight, void* workspace, size_t workspace_bytes, void* hip_stream);
+moe_status moe_block_join(const void* z, const void* stream, int stream_type, const float* post_weight, const float* gate,
+                          const float* next_weight, float scale, float eps, int T, int d, void* out, void* next, void* hip_stream);
+moe_status moe_block_join_backward(const void* d_out, const void* d_next, const void* z, const void* out, int stream_type,
+                                   const float* post_weight, const float* gate, const float* next_weight, float scale, float eps, int T, int d,
+                                   void* d_z, void* d_stream, float* d_gate, float* d_post_weight, float* d_next_weight,
+                                   void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * moe_expert_ffn_w4_sliced -- moe_expert_ffn_sliced (with the row map and router weights of moe_expert_ffn_sliced_mapped) for weights of 4 bits with
+ * one scale per group of inputs, for serving: a decoding step reads a quarter of the bytes of bf16 weights.
+ *     weight[n][k] = (code[n][k] - zero[k / group][n]) * scale[k / group][n]        (without zero points: zero = 8)
+ * No weight is rounded on the way: codes are multiplied exactly on the matrix cores, the scales multiply fp32 sums over a group.  As in
+ * moe_expert_ffn_sliced the hidden activation is rounded to bf16 once, and y to bf16.
+ *   q_gate, q_up   in  uint8 [E_loc][f][d/2], q_down uint8 [E_loc][d][f/2]: two codes per byte, the even input in the low four bits
+ *   s_gate, s_up   in  bf16 [E_loc][d/group][f], s_down bf16 [E_loc][f/group][d]   (one group's scales of all outputs side by side)
+ *   z_gate, z_up, z_down  in  uint8, laid out as the scales, the zero points 0 .. 15 (higher bits are ignored); all three or none
+ *   group          32, 64 or 128
+ *   row_map        in  int32 [offsets[last]] or NULL, row_gate float [offsets[last]] or NULL: as in moe_expert_ffn_sliced_mapped; values of row_map
+ *                      outside [0, M) read and write row 0
+ *   y              out bf16 [M][d]; rows that no schedule row names are left untouched
+ *   workspace          moe_ffn_w4_workspace_bytes(M, d, f) bytes, never less for a larger M
+ * Limits: those of moe_expert_ffn_sliced, and M * max(d, f) * 2 < 2^32 - 256; finite scales below 2^116; x, y, the codes and the workspace
+ * 16-byte aligned, scales 2-byte aligned.
+ * ------------------------------------------------------------------------------------------- */
+size_t     moe_ffn_w4_workspace_bytes(int M, int d, int f);
+moe_status moe_expert_ffn_w4_sliced(const void* x, const int32_t* offsets, int M, int S, int E_loc, int d, int f, int group,
+                                    const void* q_gate, const void* q_up, const void* q_down,
+                                    const void* s_gate, const void* s_up, const void* s_down,
+                                    const void* z_gate, const void* z_up, const void* z_down,
+                                    const int32_t* row_map, const float* row_gate,
+                                    void* y, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* ---------------------------------------------------------------------------------------------
  * moe_ffn_tile_override -- test and measurement hook, not meant for production callers.  The FFN

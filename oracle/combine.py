@@ -29,3 +29,15 @@ def combine_topk_sum(y_bits: np.ndarray, row_of: np.ndarray, gate: np.ndarray | 
             w = 1.0 if gate is None else float(np.float32(gate[t, j]))
             out[t] += w * y[r]
     return out
+
+
+def combine_topk_sum_backward(d_out: np.ndarray, y: np.ndarray, row_of: np.ndarray, gate: np.ndarray | None = None):
+    """float64 d_out [T][d] and y [R][d] -> (d_y [R][d], d_gate [T][topk]): the products of each assignment, one at a time."""
+    d_y, d_gate = np.zeros_like(y), np.zeros(row_of.shape)
+    for t in range(row_of.shape[0]):
+        for j in range(row_of.shape[1]):
+            r = int(row_of[t, j])
+            if 0 <= r < y.shape[0]:
+                d_y[r] += (1.0 if gate is None else gate[t, j]) * d_out[t]
+                d_gate[t, j] = float((d_out[t] * y[r]).sum())
+    return d_y, d_gate

@@ -23,6 +23,12 @@ MOE_DECOMP_CLEAR_TAIL = 8
 MOE_W_BF16 = 0
 MOE_W_FP8_E4M3_B128 = 1
 MOE_MAX_RANKS = 128
+MOE_T_BF16 = 0
+MOE_T_F32 = 1
+MOE_ROUTER_SOFTMAX = 0
+MOE_ROUTER_SIGMOID = 1
+MOE_ROUTER_RENORMALISE = 1
+MOE_ROUTER_MAX_TOPK = 32
 
 _STATUS = {0: "MOE_OK", -1: "MOE_ERR_INVALID_ARG", -2: "MOE_ERR_UNSUPPORTED_SHAPE", -3: "MOE_ERR_WORKSPACE",
            -4: "MOE_ERR_HIP"}
@@ -34,6 +40,9 @@ EXPORTS = [
     "moe_slice_table_rows", "moe_expert_ffn_sliced_mapped", "moe_ffn_tile_override",
     "moe_slice_table_static", "moe_decompose_profile", "moe_combine_topk_sum",
     "moe_ffn_backward_workspace_bytes", "moe_expert_ffn_backward_sliced", "moe_probe_mfma_bf16",
+    "moe_combine_backward_workspace_bytes", "moe_combine_topk_sum_backward", "moe_router_topk", "moe_router_topk_backward",
+    "moe_block_backward_workspace_bytes", "moe_block_norm", "moe_block_norm_backward", "moe_block_join", "moe_block_join_backward",
+    "moe_ffn_w4_workspace_bytes", "moe_expert_ffn_w4_sliced",
 ]
 
 _lib = None
@@ -115,6 +124,29 @@ def load():
     L.moe_expert_ffn_backward_sliced.restype = ci
     L.moe_combine_topk_sum.argtypes = [vp, vp, vp, ci, ci, ci, ci, vp, vp]
     L.moe_combine_topk_sum.restype = ci
+    cf = ctypes.c_float
+    L.moe_combine_backward_workspace_bytes.argtypes = [ci]
+    L.moe_combine_backward_workspace_bytes.restype = sz
+    L.moe_combine_topk_sum_backward.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, vp, vp, vp, sz, vp]
+    L.moe_combine_topk_sum_backward.restype = ci
+    L.moe_router_topk.argtypes = [vp, ci, ci, ci, ci, ci, ci, cf, vp, vp, vp]
+    L.moe_router_topk.restype = ci
+    L.moe_router_topk_backward.argtypes = [vp, vp, ci, vp, ci, ci, ci, ci, ci, cf, vp, vp]
+    L.moe_router_topk_backward.restype = ci
+    L.moe_block_backward_workspace_bytes.argtypes = [ci, ci]
+    L.moe_block_backward_workspace_bytes.restype = sz
+    L.moe_block_norm.argtypes = [vp, ci, vp, cf, ci, ci, vp, vp]
+    L.moe_block_norm.restype = ci
+    L.moe_block_norm_backward.argtypes = [vp, vp, ci, vp, vp, cf, ci, ci, vp, vp, vp, sz, vp]
+    L.moe_block_norm_backward.restype = ci
+    L.moe_block_join.argtypes = [vp, vp, ci, vp, vp, vp, cf, cf, ci, ci, vp, vp, vp]
+    L.moe_block_join.restype = ci
+    L.moe_block_join_backward.argtypes = [vp, vp, vp, vp, ci, vp, vp, vp, cf, cf, ci, ci, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.moe_block_join_backward.restype = ci
+    L.moe_ffn_w4_workspace_bytes.argtypes = [ci, ci, ci]
+    L.moe_ffn_w4_workspace_bytes.restype = sz
+    L.moe_expert_ffn_w4_sliced.argtypes = [vp, vp, ci, ci, ci, ci, ci, ci] + [vp] * 13 + [sz, vp]
+    L.moe_expert_ffn_w4_sliced.restype = ci
     L.moe_probe_mfma_bf16.argtypes = [ci, ci, ci, vp, vp]
     L.moe_probe_mfma_bf16.restype = ci
     L.moe_ffn_tile_override.argtypes = [ci, ci, ci]
@@ -418,6 +450,212 @@ def moe_combine_topk_sum(y, row_of, gate=None, out=None):
     _check(load().moe_combine_topk_sum(_ptr(y), _ptr(row_of), _ptr(gate), T, topk, d, R, _ptr(out), _stream()),
            "moe_combine_topk_sum")
     return out
+
+
+# --------------------------------------------------------------------------------------------- around the experts
+def _operands(what, wanted):
+    """wanted: (name, tensor or None, dtype or allowed dtypes, shape).  All tensors contiguous, of that type and shape, on one device, which is
+    made current for the call; returns the context that does so and the handle of the device's stream."""
+    import torch
+    device = None
+    for name, t, dtype, shape in wanted:
+        if t is None:
+            continue
+        if not t.is_cuda or not t.is_contiguous() or (t.dtype not in dtype if isinstance(dtype, tuple) else t.dtype != dtype) or tuple(t.shape) != shape:
+            raise MoeError("%s: %s must be a contiguous CUDA tensor of dtype %s and shape %s" % (what, name, dtype, list(shape)))
+        if device is None:
+            device = t.get_device()
+        elif t.get_device() != device:
+            raise MoeError("%s: %s is on another device" % (what, name))
+    return device
+
+
+def _on(device, what, call):
+    """call(stream handle) on the current stream of `device`."""
+    import torch
+    if device != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            rc = call(torch.cuda.current_stream(device).cuda_stream)
+    else:
+        rc = call(torch.cuda.current_stream(device).cuda_stream)
+    _check(rc, what)
+
+
+def _two(t, what, name):
+    if t is None or t.dim() != 2:
+        raise MoeError("%s: %s must be a tensor of two dimensions" % (what, name))
+    return t.shape
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _bytes(need, workspace, device_of, what):
+    import torch
+    if workspace is None:
+        return torch.empty((max(need, 1),), dtype=torch.uint8, device=device_of.device)
+    if not workspace.is_cuda or not workspace.is_contiguous() or workspace.dtype != torch.uint8 or workspace.get_device() != device_of.get_device():
+        raise MoeError("%s: workspace must be a contiguous uint8 tensor on the device of the operands" % what)
+    return workspace
+
+
+def moe_block_norm(x, weight, eps: float = 1e-6, out=None):
+    """x bf16 or float32 [T][d], weight float32 [d] -> out bf16 [T][d] = x / rms(x) * weight."""
+    import torch
+    what = "moe_block_norm"
+    T, d = _two(x, what, "x")
+    if out is None:
+        out = torch.empty((T, d), dtype=torch.bfloat16, device=x.device)
+    dev = _operands(what, (("x", x, (torch.bfloat16, torch.float32), (T, d)), ("weight", weight, torch.float32, (d,)), ("out", out, torch.bfloat16, (T, d))))
+    _on(dev, what, lambda s: load().moe_block_norm(x.data_ptr(), int(x.dtype == torch.float32), _at(weight), eps, T, d, out.data_ptr(), s))
+    return out
+
+
+def moe_block_norm_backward(d_out, x, weight, eps: float = 1e-6, d_stream=None, workspace=None):
+    """d_out bf16 [T][d], x and d_stream (or None) bf16 or float32 [T][d], weight float32 [d] -> dict(d_x like x = d_stream + the norm's gradient, d_weight)."""
+    import torch
+    what = "moe_block_norm_backward"
+    T, d = _two(x, what, "x")
+    dev = _operands(what, (("d_out", d_out, torch.bfloat16, (T, d)), ("x", x, (torch.bfloat16, torch.float32), (T, d)), ("weight", weight, torch.float32, (d,)),
+                           ("d_stream", d_stream, x.dtype, (T, d))))
+    o = dict(d_x=torch.empty_like(x), d_weight=torch.empty_like(weight))
+    workspace = _bytes(int(load().moe_block_backward_workspace_bytes(T, d)), workspace, x, what)
+    _on(dev, what, lambda s: load().moe_block_norm_backward(_at(d_out), x.data_ptr(), int(x.dtype == torch.float32), _at(weight), _at(d_stream), eps, T, d,
+                                                            o["d_x"].data_ptr(), o["d_weight"].data_ptr(), workspace.data_ptr(), workspace.numel(), s))
+    return o
+
+
+def moe_block_join(z, stream, post_weight=None, gate=None, next_weight=None, scale: float = 1.0, eps: float = 1e-6, out=None, next_out=None):
+    """z bf16 [T][d] (the block's result), stream bf16 or float32 [T][d], weights float32 [d], gate float32 [T] ->
+    (out like stream = scale * stream + gate * norm(z), next bf16 = norm(out) or None without next_weight)."""
+    import torch
+    what = "moe_block_join"
+    T, d = _two(z, what, "z")
+    if out is None:
+        out = torch.empty_like(stream)
+    if next_out is None and next_weight is not None:
+        next_out = torch.empty_like(z)
+    stream_types = (torch.bfloat16, torch.float32)
+    dev = _operands(what, (("z", z, torch.bfloat16, (T, d)), ("stream", stream, stream_types, (T, d)), ("post_weight", post_weight, torch.float32, (d,)),
+                           ("gate", gate, torch.float32, (T,)), ("next_weight", next_weight, torch.float32, (d,)), ("out", out, stream.dtype, (T, d)),
+                           ("next_out", next_out, torch.bfloat16, (T, d))))
+    _on(dev, what, lambda s: load().moe_block_join(z.data_ptr(), stream.data_ptr(), int(stream.dtype == torch.float32), _at(post_weight), _at(gate), _at(next_weight),
+                                                   scale, eps, T, d, out.data_ptr(), _at(next_out), s))
+    return out, next_out
+
+
+def moe_block_join_backward(d_out, d_next, z, out, post_weight=None, gate=None, next_weight=None, scale: float = 1.0, eps: float = 1e-6,
+                            workspace=None):
+    """d_out (like out, or None), d_next (bf16, with next_weight), z bf16 and out [T][d] as the forward call took and returned them ->
+    dict(d_z, d_stream, d_gate, d_post_weight, d_next_weight); the last three are None where their input is."""
+    import torch
+    what = "moe_block_join_backward"
+    T, d = _two(z, what, "z")
+    stream_types = (torch.bfloat16, torch.float32)
+    if out is None:
+        raise MoeError("%s: out is required" % what)
+    dev = _operands(what, (("d_out", d_out, out.dtype, (T, d)), ("d_next", d_next, torch.bfloat16, (T, d)), ("z", z, torch.bfloat16, (T, d)),
+                           ("out", out, stream_types, (T, d)), ("post_weight", post_weight, torch.float32, (d,)), ("gate", gate, torch.float32, (T,)),
+                           ("next_weight", next_weight, torch.float32, (d,))))
+    like = lambda t: None if t is None else torch.empty_like(t)                              # noqa: E731
+    o = dict(d_z=torch.empty_like(z), d_stream=torch.empty_like(out), d_gate=like(gate), d_post_weight=like(post_weight), d_next_weight=like(next_weight))
+    workspace = _bytes(int(load().moe_block_backward_workspace_bytes(T, d)), workspace, z, what)
+    _on(dev, what, lambda s: load().moe_block_join_backward(_at(d_out), _at(d_next), z.data_ptr(), out.data_ptr(), int(out.dtype == torch.float32), _at(post_weight),
+                                                            _at(gate), _at(next_weight), scale, eps, T, d, o["d_z"].data_ptr(), o["d_stream"].data_ptr(),
+                                                            _at(o["d_gate"]), _at(o["d_post_weight"]), _at(o["d_next_weight"]), workspace.data_ptr(),
+                                                            workspace.numel(), s))
+    return o
+
+
+_SCORES = {"softmax": MOE_ROUTER_SOFTMAX, "sigmoid": MOE_ROUTER_SIGMOID}
+
+
+def _score(score, what):
+    if score not in _SCORES:
+        raise MoeError("%s: score must be 'softmax' or 'sigmoid'" % what)
+    return _SCORES[score]
+
+
+def moe_router_topk(logits, topk: int, score: str = "softmax", renormalise: bool = True, scale: float = 1.0, ids=None, gates=None):
+    """logits bf16 or float32 [T][E] -> (ids int32 [T][topk], gates float32 [T][topk]); -inf masks an expert, a slot without expert is (-1, 0)."""
+    import torch
+    what = "moe_router_topk"
+    T, E = _two(logits, what, "logits")
+    if ids is None:
+        ids = torch.empty((T, topk), dtype=torch.int32, device=logits.device)
+    if gates is None:
+        gates = torch.empty((T, topk), dtype=torch.float32, device=logits.device)
+    dev = _operands(what, (("logits", logits, (torch.bfloat16, torch.float32), (T, E)), ("ids", ids, torch.int32, (T, topk)), ("gates", gates, torch.float32, (T, topk))))
+    sc = _score(score, what)
+    _on(dev, what, lambda s: load().moe_router_topk(logits.data_ptr(), int(logits.dtype == torch.float32), T, E, topk, sc, MOE_ROUTER_RENORMALISE if renormalise else 0,
+                                                    scale, ids.data_ptr(), gates.data_ptr(), s))
+    return ids, gates
+
+
+def moe_router_topk_backward(d_gates, logits, ids, score: str = "softmax", renormalise: bool = True, scale: float = 1.0, d_logits=None):
+    """d_gates float32 [T][topk], logits and ids as the forward call took and returned them -> d_logits [T][E] in the type of the logits."""
+    import torch
+    what = "moe_router_topk_backward"
+    T, E = _two(logits, what, "logits")
+    topk = _two(ids, what, "ids")[1]
+    if d_logits is None:
+        d_logits = torch.empty_like(logits)
+    dev = _operands(what, (("d_gates", d_gates, torch.float32, (T, topk)), ("logits", logits, (torch.bfloat16, torch.float32), (T, E)), ("ids", ids, torch.int32, (T, topk)),
+                           ("d_logits", d_logits, logits.dtype, (T, E))))
+    sc = _score(score, what)
+    _on(dev, what, lambda s: load().moe_router_topk_backward(d_gates.data_ptr(), logits.data_ptr(), int(logits.dtype == torch.float32), ids.data_ptr(), T, E, topk, sc,
+                                                             MOE_ROUTER_RENORMALISE if renormalise else 0, scale, d_logits.data_ptr(), s))
+    return d_logits
+
+
+def moe_combine_topk_sum_backward(d_out, y, row_of, gate=None, workspace=None):
+    """d_out bf16 [T][d], y bf16 [R][d], row_of int32 [T][topk], gate float32 [T][topk] or None -> dict(d_y [R][d], d_gate [T][topk] or None)."""
+    import torch
+    what = "moe_combine_topk_sum_backward"
+    T, topk = _two(row_of, what, "row_of")
+    R, d = _two(y, what, "y")
+    dev = _operands(what, (("d_out", d_out, torch.bfloat16, (T, d)), ("y", y, torch.bfloat16, (R, d)), ("row_of", row_of, torch.int32, (T, topk)),
+                           ("gate", gate, torch.float32, (T, topk))))
+    o = dict(d_y=torch.empty_like(y), d_gate=None if gate is None else torch.empty_like(gate))
+    workspace = _bytes(int(load().moe_combine_backward_workspace_bytes(R)), workspace, y, what)
+    _on(dev, what, lambda s: load().moe_combine_topk_sum_backward(_at(d_out), y.data_ptr(), row_of.data_ptr(), _at(gate), T, topk, d, R, o["d_y"].data_ptr(),
+                                                                  _at(o["d_gate"]), workspace.data_ptr(), workspace.numel(), s))
+    return o
+
+
+def moe_ffn_w4_workspace_bytes(M: int, d: int, f: int) -> int:
+    return int(load().moe_ffn_w4_workspace_bytes(M, d, f))
+
+
+def moe_expert_ffn_w4_sliced(x, offsets, S: int, E_loc: int, q_gate, q_up, q_down, s_gate, s_up, s_down, z_gate=None, z_up=None, z_down=None,
+                             row_map=None, row_gate=None, y=None, workspace=None):
+    """x bf16 [M][d]; offsets int32 [S*E_loc+1]; codes uint8 q_gate, q_up [E_loc][f][d/2], q_down [E_loc][d][f/2] (even input in the low four bits); scales bf16
+    [E_loc][d/group][f] and [E_loc][f/group][d]; zero points uint8 like the scales, or None (= 8); row_map int32 [M] and row_gate float32 [M]
+    (entries behind the schedule's last row are not read) -> y bf16 [M][d]."""
+    import torch
+    what = "moe_expert_ffn_w4_sliced"
+    M, d = _two(x, what, "x")
+    if s_gate is None or s_gate.dim() != 3 or q_gate is None or q_gate.dim() != 3 or s_gate.shape[1] < 1:
+        raise MoeError("%s: codes and scales must be tensors of three dimensions" % what)
+    f, group = q_gate.shape[1], d // s_gate.shape[1]
+    if group not in (32, 64, 128) or d % group or f % group:
+        raise MoeError("%s: scales must be one per group of 32, 64 or 128 inputs" % what)
+    if (z_gate is None) != (z_up is None) or (z_gate is None) != (z_down is None):
+        raise MoeError("%s: zero points are given for all three weights or for none" % what)
+    if y is None:
+        y = torch.empty_like(x)
+    up, down = (E_loc, d // group, f), (E_loc, f // group, d)
+    dev = _operands(what, (("x", x, torch.bfloat16, (M, d)), ("offsets", offsets, torch.int32, (S * E_loc + 1,)), ("y", y, torch.bfloat16, (M, d)),
+                           ("q_gate", q_gate, torch.uint8, (E_loc, f, d // 2)), ("q_up", q_up, torch.uint8, (E_loc, f, d // 2)),
+                           ("q_down", q_down, torch.uint8, (E_loc, d, f // 2)), ("s_gate", s_gate, torch.bfloat16, up), ("s_up", s_up, torch.bfloat16, up),
+                           ("s_down", s_down, torch.bfloat16, down), ("z_gate", z_gate, torch.uint8, up), ("z_up", z_up, torch.uint8, up),
+                           ("z_down", z_down, torch.uint8, down), ("row_map", row_map, torch.int32, (M,)), ("row_gate", row_gate, torch.float32, (M,))))
+    workspace = _bytes(moe_ffn_w4_workspace_bytes(M, d, f), workspace, x, what)
+    _on(dev, what, lambda s: load().moe_expert_ffn_w4_sliced(
+        x.data_ptr(), offsets.data_ptr(), M, S, E_loc, d, f, group, q_gate.data_ptr(), q_up.data_ptr(), q_down.data_ptr(), s_gate.data_ptr(), s_up.data_ptr(),
+        s_down.data_ptr(), _at(z_gate), _at(z_up), _at(z_down), _at(row_map), _at(row_gate), y.data_ptr(), workspace.data_ptr(), workspace.numel(), s))
+    return y
 
 
 def moe_probe_mfma_bf16(data: int, iters: int, workgroups: int, sink=None):

@@ -5,7 +5,7 @@
 // columns (16 bytes), issues the loads of all its slots before it adds (the bytes in flight per thread are what fills
 // the memory pipeline) and accumulates in fp32 in slot order.  Result rows are read once by the whole grid, so the loads
 // are non-temporal.
-#include "common.hpp"
+#include "lanes.hpp"
 #include <algorithm>
 
 namespace {
@@ -119,4 +119,207 @@ extern "C" moe_status moe_combine_topk_sum(const void* y, const int32_t* row_of,
         default: hipLaunchKernelGGL(combine_kernel<0>, grid, dim3(CB_THREADS), 0, s, yy, row_of, gate, T, topk, d, R, oo); break;
     }
     return k.done();
+}
+
+// ---------------------------------------------------------------------------------- gradients of the combine
+// moe_combine_topk_sum_backward: d_y[row_of[t][j]] += gate[t][j] d_out[t], d_gate[t][j] = d_out[t] . y[row_of[t][j]].
+// HBM bound: d_out is read once, y read and d_y written once.  A workgroup takes a token: its threads hold d_out[t] (8 columns a
+// step) and walk the token's rows, whose loads go out together.  Nearly always a row belongs to one assignment and is written right here.  A row that
+// several assignments name (counted beforehand) is left to combine_backward_rest_kernel, which adds them up in the order of the assignments, and so
+// is a row that none names, whose gradient is zero.
+namespace {
+
+constexpr int CBB_MAX_COLUMNS = 16384;
+
+// uses[r] = number of assignments that name row r
+__global__ __launch_bounds__(256)
+void combine_clear_kernel(int32_t* __restrict__ uses, int R) {
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < R; i += (long long)gridDim.x * 256) uses[i] = 0;
+}
+__global__ __launch_bounds__(256)
+void combine_count_kernel(const int32_t* __restrict__ row_of, int n, int R, int32_t* __restrict__ uses) {
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+        const int r = row_of[i];
+        if ((unsigned)r < (unsigned)R) atomicAdd(uses + r, 1);
+    }
+}
+
+struct CombineBackwardArgs {
+    const __bf16 *d_out, *y;
+    const int32_t* row_of;
+    const float* gate;
+    const int32_t* uses;
+    __bf16* d_y;
+    float* d_gate;
+    int T, topk, d, R;
+};
+
+__device__ __forceinline__ void cb_widen(cb_u32x4 r, float (&v)[8]) {
+    const cb_bf16x8 b = __builtin_bit_cast(cb_bf16x8, r);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) v[c] = (float)b[c];
+}
+__device__ __forceinline__ cb_u32x4 cb_scaled(const float (&v)[8], float w) {
+    cb_bf16x8 o;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) o[c] = (__bf16)(w * v[c]);
+    return __builtin_bit_cast(cb_u32x4, o);
+}
+
+// NT threads per token, NV steps of NT * 8 columns, J rows of y in flight at once
+template <int NT, int NV, int J>
+__global__ __launch_bounds__(NT == 64 ? 256 : NT)
+void combine_backward_kernel(CombineBackwardArgs a) {
+    constexpr int PER = NT == 64 ? 4 : 1;
+    __shared__ float s_sum[2 * J * (NT / 64)];
+    int half = 0;
+    const int tid = threadIdx.x % NT;
+    const long long t = (long long)blockIdx.x * PER + (int)threadIdx.x / NT;
+    if (t >= a.T) return;                                                 // (a whole wavefront, which meets no barrier if NT is 64)
+    cb_u32x4 raw[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int col = (v * NT + tid) * 8;
+        raw[v] = cb_u32x4{0u, 0u, 0u, 0u};
+        if (col < a.d) raw[v] = *reinterpret_cast<const cb_u32x4*>(a.d_out + (size_t)t * a.d + col);
+    }
+    for (int j0 = 0; j0 < a.topk; j0 += J) {
+        int row[J];
+        bool alone[J];
+        float w[J], dot[J];
+        cb_u32x4 y[J][NV];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const size_t at = (size_t)t * a.topk + min(j0 + j, a.topk - 1);
+            row[j] = j0 + j < a.topk ? a.row_of[at] : -1;
+            if ((unsigned)row[j] >= (unsigned)a.R) row[j] = -1;
+            w[j] = a.gate && row[j] >= 0 ? a.gate[at] : 1.0f;
+            alone[j] = row[j] >= 0 && a.uses[row[j]] == 1;
+            dot[j] = 0.0f;
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int col = (v * NT + tid) * 8;
+                y[j][v] = cb_u32x4{0u, 0u, 0u, 0u};
+                if (a.d_gate && row[j] >= 0 && col < a.d) y[j][v] = __builtin_nontemporal_load(reinterpret_cast<const cb_u32x4*>(a.y + (size_t)row[j] * a.d + col));
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int col = (v * NT + tid) * 8;
+            float g[8];
+            cb_widen(raw[v], g);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                float b[8];
+                cb_widen(y[j][v], b);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) dot[j] = __builtin_fmaf(g[c], b[c], dot[j]);
+                if (alone[j] && col < a.d)
+                    __builtin_nontemporal_store(cb_scaled(g, w[j]), reinterpret_cast<cb_u32x4*>(a.d_y + (size_t)row[j] * a.d + col));
+            }
+        }
+        if (a.d_gate) {
+            moe::workgroup_sums<NT>(dot, s_sum, half);
+            if (tid < J && j0 + tid < a.topk) {
+                float mine = 0.0f;
+#pragma unroll
+                for (int j = 0; j < J; ++j) mine = tid == j && row[j] >= 0 ? dot[j] : mine;      // a dropped assignment's weight has no effect
+                a.d_gate[(size_t)t * a.topk + j0 + tid] = mine;
+            }
+        }
+    }
+}
+
+// rows that no assignment names, or several do: those are found by going through all assignments, 256 at a time, and added in their order
+__global__ __launch_bounds__(256)
+void combine_backward_rest_kernel(CombineBackwardArgs a) {
+    __shared__ unsigned long long s_hit[4];
+    const int wave = threadIdx.x >> 6, n = a.T * a.topk;
+    for (long long r = blockIdx.x; r < a.R; r += gridDim.x) {
+        const int uses = a.uses[r];                                        // (the same for the whole workgroup)
+        if (uses == 1) continue;
+        if (uses == 0) {
+            for (int col = threadIdx.x * 8; col < a.d; col += 256 * 8) *reinterpret_cast<cb_u32x4*>(a.d_y + (size_t)r * a.d + col) = cb_u32x4{0u, 0u, 0u, 0u};
+            continue;
+        }
+        for (int c0 = 0; c0 < a.d; c0 += 256 * 8) {
+            const int col = c0 + threadIdx.x * 8;
+            float sum[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) sum[c] = 0.0f;
+            int left = uses;
+            for (long long i0 = 0; i0 < n && left > 0; i0 += 256) {
+                const long long i = i0 + threadIdx.x;
+                const unsigned long long hit = __ballot(i < n && a.row_of[i < n ? i : 0] == r);
+                if ((threadIdx.x & 63) == 0) s_hit[wave] = hit;
+                __syncthreads();
+                for (int w = 0; w < 4; ++w) {
+                    unsigned long long h = s_hit[w];
+                    while (h) {
+                        const int at = (int)i0 + w * 64 + __builtin_ctzll(h);
+                        h &= h - 1;
+                        --left;
+                        if (col < a.d) {
+                            const float g = a.gate ? a.gate[at] : 1.0f;
+                            float v[8];
+                            cb_widen(*reinterpret_cast<const cb_u32x4*>(a.d_out + (size_t)(at / a.topk) * a.d + col), v);
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) sum[c] = __builtin_fmaf(g, v[c], sum[c]);
+                        }
+                    }
+                }
+                __syncthreads();
+            }
+            if (col < a.d) *reinterpret_cast<cb_u32x4*>(a.d_y + (size_t)r * a.d + col) = cb_scaled(sum, 1.0f);
+        }
+    }
+}
+
+template <int NT, int NV, int J> void launch_combine_backward(const CombineBackwardArgs& a, hipStream_t s) {
+    constexpr int PER = NT == 64 ? 4 : 1;
+    hipLaunchKernelGGL((combine_backward_kernel<NT, NV, J>), dim3((unsigned)((a.T - 1) / PER + 1)), dim3(NT == 64 ? 256 : NT), 0, s, a);
+}
+template <int NT, int NV> void launch_combine_backward(const CombineBackwardArgs& a, hipStream_t s) {
+    if (a.topk == 1) launch_combine_backward<NT, NV, 1>(a, s);
+    else if (a.topk == 2) launch_combine_backward<NT, NV, 2>(a, s);
+    else launch_combine_backward<NT, NV, 4>(a, s);
+}
+
+}  // namespace
+
+extern "C" size_t moe_combine_backward_workspace_bytes(int R) { return R < 0 ? 0 : (((size_t)R * sizeof(int32_t)) + 255) & ~(size_t)255; }
+
+extern "C" moe_status moe_combine_topk_sum_backward(const void* d_out, const void* y, const int32_t* row_of, const float* gate, int T, int topk, int d, int R,
+                                                    void* d_y, float* d_gate, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (T < 0 || topk < 1 || d < 1 || R < 0) return MOE_ERR_INVALID_ARG;
+    if (d % 8 != 0 || d > CBB_MAX_COLUMNS || T > 0x7FFFFFFF / topk) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if ((T > 0 && (!d_out || !row_of || (gate && !d_gate))) || (R > 0 && (!y || !d_y)) || (!gate && d_gate)) return MOE_ERR_INVALID_ARG;
+    if ((((uintptr_t)d_out | (uintptr_t)y | (uintptr_t)d_y | (uintptr_t)workspace) & 15) != 0) return MOE_ERR_INVALID_ARG;
+    if (R > 0 && (!workspace || workspace_bytes < moe_combine_backward_workspace_bytes(R))) return MOE_ERR_WORKSPACE;
+    hipStream_t s = (hipStream_t)hip_stream;
+    const int cus = moe::compute_units(), n = T * topk;
+    CombineBackwardArgs a = {(const __bf16*)d_out, (const __bf16*)y, row_of, gate, (const int32_t*)workspace, (__bf16*)d_y, d_gate, T, topk, d, R};
+    const auto blocks = [&](int items) { return dim3((unsigned)std::min((items - 1) / 256 + 1, cus * 8)); };
+    if (R > 0) {
+        moe::LaunchScope k("combine_count_kernel", s);
+        hipLaunchKernelGGL(combine_clear_kernel, blocks(R), dim3(256), 0, s, (int32_t*)workspace, R);
+        if (n > 0) hipLaunchKernelGGL(combine_count_kernel, blocks(n), dim3(256), 0, s, row_of, n, R, (int32_t*)workspace);
+        if (const moe_status st = k.done()) return st;
+    }
+    if (T > 0) {
+        moe::LaunchScope k("combine_backward_kernel", s);
+        if (d <= 512) launch_combine_backward<64, 1>(a, s);
+        else if (d <= 1024) launch_combine_backward<64, 2>(a, s);
+        else if (d <= 2048) launch_combine_backward<256, 1>(a, s);
+        else if (d <= 4096) launch_combine_backward<256, 2>(a, s);
+        else if (d <= 8192) launch_combine_backward<512, 2>(a, s);
+        else launch_combine_backward<1024, 2>(a, s);
+        if (const moe_status st = k.done()) return st;
+    }
+    if (R > 0) {
+        moe::LaunchScope k("combine_backward_rest_kernel", s);
+        hipLaunchKernelGGL(combine_backward_rest_kernel, dim3((unsigned)std::min(R, cus * 8)), dim3(256), 0, s, a);
+        if (const moe_status st = k.done()) return st;
+    }
+    return MOE_OK;
 }

@@ -30,6 +30,19 @@ struct LaunchScope {
     }
 };
 
+// compute units of the current device (256 where it cannot be asked), looked up once per device
+inline int compute_units() {
+    static std::atomic<int> known[64];
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
+    int n = known[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
+        known[dev].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
 // "Done once per device" for set-up that HIP keeps per device (function attributes): bit d = done on device d.
 struct DeviceOnce {
     std::atomic<unsigned long long> done{0};

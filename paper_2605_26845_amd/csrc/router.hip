@@ -1,0 +1,354 @@
+// moe_router_topk and its backward pass: the router of a MoE block (Section 2.1: each token is sent to its top-k experts), from logits to
+// the expert ids that the histogram counts and the weights that the combine takes.
+//
+// LANES neighbouring lanes own a token and VPL neighbouring experts each: the logits are read once with wide loads.  Every lane sorts
+// its experts by (logit, lower index first); the largest head of all lanes is taken topk times, and the lane that held it moves its list up.
+// (More than 8 experts per lane are looked through each time instead: sorting them is a quadratic number of exchanges.)
+// Neither the order of the lanes nor any atomic decides a tie: equal logits go to the lower index.
+#include "lanes.hpp"
+#include <algorithm>
+
+namespace {
+
+constexpr int ROUTER_THREADS = 256;
+
+typedef __attribute__((ext_vector_type(4))) unsigned int r_u32x4;
+typedef __attribute__((ext_vector_type(4))) float r_f32x4;
+
+struct RouterArgs {
+    const void* logits;
+    const int32_t* ids_in;                     // backward
+    const float* d_gates;                      // backward
+    int32_t* ids;
+    float* gates;
+    void* d_logits;
+    float scale;
+    int T, E, topk, score, renormalise;
+};
+
+// the first expert of this lane is e0; experts past the end and NaN count as masked
+template <bool F32, int VPL, bool WIDE> __device__ __forceinline__ void read_logits(const void* p, size_t at, int e0, int E, float (&v)[VPL]) {
+    constexpr int PIECE = F32 ? 4 : 8;                                     // values per 16 bytes
+    if constexpr (WIDE && VPL % PIECE == 0) {
+#pragma unroll
+        for (int i = 0; i < VPL; i += PIECE) {
+            if (e0 + i < E) {                                             // (E is a multiple of PIECE here)
+                if constexpr (F32) {
+                    const r_f32x4 r = *reinterpret_cast<const r_f32x4*>((const float*)p + at + i);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) v[i + c] = r[c];
+                } else {
+                    const r_u32x4 r = *reinterpret_cast<const r_u32x4*>((const __bf16*)p + at + i);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        v[i + 2 * c] = __builtin_bit_cast(float, r[c] << 16);
+                        v[i + 2 * c + 1] = __builtin_bit_cast(float, r[c] & 0xFFFF0000u);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < PIECE; ++c) v[i + c] = -__builtin_inff();
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) {
+            v[i] = -__builtin_inff();
+            if (e0 + i < E) v[i] = F32 ? ((const float*)p)[at + i] : (float)((const __bf16*)p)[at + i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) v[i] = v[i] != v[i] ? -__builtin_inff() : v[i];
+}
+
+// a float as an unsigned number of the same order; 0 and -0 are the same, and the masked ones (-inf) become 0
+__device__ __forceinline__ unsigned int order_key(float x) {
+    const unsigned int u = __builtin_bit_cast(unsigned int, x + 0.0f);
+    return x == -__builtin_inff() ? 0u : ((u & 0x80000000u) ? ~u : u | 0x80000000u);
+}
+__device__ __forceinline__ float key_value(unsigned int k) {
+    return k == 0u ? -__builtin_inff() : __builtin_bit_cast(float, (k & 0x80000000u) ? k & 0x7FFFFFFFu : ~k);
+}
+
+__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
+// exp(x - top), top being at least x; equal infinities are as far apart as equal numbers
+__device__ __forceinline__ float exp_below(float x, float top) { return x == top ? 1.0f : expf(x - top); }
+
+// sigmoid(x) / sigmoid(top) for x <= top, also where both are too small for a float
+__device__ __forceinline__ float sigmoid_ratio(float x, float top) {
+    const float ex = expf(-__builtin_fabsf(x)), et = expf(-__builtin_fabsf(top));
+    return exp_below(fminf(x, 0.0f), fminf(top, 0.0f)) * (1.0f + et) / (1.0f + ex);
+}
+
+template <bool F32, int LANES, int VPL, bool WIDE>
+__global__ __launch_bounds__(ROUTER_THREADS)
+void router_topk_kernel(RouterArgs a) {
+    const int sub = threadIdx.x % LANES;
+    const long long t = (long long)blockIdx.x * (ROUTER_THREADS / LANES) + threadIdx.x / LANES;
+    const bool live = t < a.T;                                             // (lanes of other tokens take part in the wavefront's exchanges)
+    const int e0 = sub * VPL;
+    float v[VPL];
+    if (live) read_logits<F32, VPL, WIDE>(a.logits, (size_t)t * a.E + e0, e0, a.E, v);
+    else {
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) v[i] = -__builtin_inff();
+    }
+    // this lane's experts in falling order (a sort by exchanges of neighbours keeps equal ones in the order of their index)
+    constexpr bool SORTED = VPL <= 8;
+    unsigned int key[VPL], idx[SORTED ? VPL : 1], head, head_idx;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) key[i] = order_key(v[i]);
+    auto look = [&]() __attribute__((always_inline)) {                     // the first of this lane's largest
+        head = key[0]; head_idx = (unsigned)e0;
+#pragma unroll
+        for (int i = 1; i < VPL; ++i) {
+            const bool more = key[i] > head;
+            head = more ? key[i] : head;
+            head_idx = more ? (unsigned)(e0 + i) : head_idx;
+        }
+    };
+    if constexpr (SORTED) {
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) idx[i] = (unsigned)(e0 + i);
+#pragma unroll
+        for (int p = 0; p < VPL - 1; ++p)
+#pragma unroll
+            for (int i = VPL - 1; i > p; --i) {
+                const bool up = key[i] > key[i - 1];
+                const unsigned int k = key[i], x = idx[i];
+                key[i] = up ? key[i - 1] : k; idx[i] = up ? idx[i - 1] : x;
+                key[i - 1] = up ? k : key[i - 1]; idx[i - 1] = up ? x : idx[i - 1];
+            }
+        head = key[0]; head_idx = idx[0];
+    } else {
+        look();
+    }
+    const float top = key_value(moe::lanes_max<LANES>(head));
+    float all = 0.0f;                                                      // sum of exp(logit - top) over all experts
+    if (a.score == MOE_ROUTER_SOFTMAX && !a.renormalise) {
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) all += v[i] == -__builtin_inff() ? 0.0f : exp_below(v[i], top);
+        all = moe::lanes_sum<LANES>(all);
+    }
+    // lane j % LANES keeps slot j's choice
+    constexpr int KEEP = (MOE_ROUTER_MAX_TOPK + LANES - 1) / LANES;
+    unsigned int got_key[KEEP], got_idx[KEEP];
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) got_key[i] = got_idx[i] = 0u;
+    for (int j = 0; j < a.topk; ++j) {
+        const unsigned int best = moe::lanes_max<LANES>(head);
+        const unsigned int who = moe::lanes_min<LANES>(head == best ? head_idx : 0xFFFFFFFFu);
+        if (sub == j % LANES) {
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i)
+                if (i == j / LANES) { got_key[i] = best; got_idx[i] = who; }
+        }
+        const bool mine = head_idx == who;                                // (heads of zero are masked experts, whatever their index)
+        if constexpr (SORTED) {
+#pragma unroll
+            for (int i = 0; i + 1 < VPL; ++i) { key[i] = mine ? key[i + 1] : key[i]; idx[i] = mine ? idx[i + 1] : idx[i]; }
+            if (mine) { key[VPL - 1] = 0u; idx[VPL - 1] = 0xFFFFFFFEu; }
+            head = key[0]; head_idx = idx[0];
+        } else {
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) key[i] = mine && who == (unsigned)(e0 + i) ? 0u : key[i];
+            look();
+        }
+    }
+    float w[KEEP], sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) {
+        const float x = key_value(got_key[i]);
+        w[i] = 0.0f;
+        if (got_key[i] != 0u) {
+            if (a.score == MOE_ROUTER_SOFTMAX) w[i] = exp_below(x, top);
+            else w[i] = a.renormalise ? sigmoid_ratio(x, top) : sigmoid(x);
+        }
+        sum += w[i];
+    }
+    if (a.renormalise) all = moe::lanes_sum<LANES>(sum);
+    const float by = (a.renormalise || a.score == MOE_ROUTER_SOFTMAX) ? (all > 0.0f ? a.scale / all : 0.0f) : a.scale;
+    if (live) {
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) {
+            const int j = i * LANES + sub;
+            if (j < a.topk) {
+                a.ids[(size_t)t * a.topk + j] = got_key[i] != 0u ? (int32_t)got_idx[i] : -1;
+                a.gates[(size_t)t * a.topk + j] = w[i] * by;
+            }
+        }
+    }
+}
+
+// One wavefront per token; a lane writes VPL neighbouring logits' gradients at a time.  With G_j = scale d_gate_j over the slots whose expert is in range:
+//   softmax                 d_l[e] = p_e (sum of G_j with id_j = e  -  sum_j G_j p_j)
+//   renormalised (w_j sum to one over the slots)      d_l[id_j] += w_j (1 - sigmoid(l_j) for sigmoid scores, else 1) (G_j - sum_k G_k w_k)
+//   sigmoid                 d_l[id_j] += G_j s_j (1 - s_j)
+template <bool F32, bool WIDE>
+__global__ __launch_bounds__(ROUTER_THREADS)
+void router_backward_kernel(RouterArgs a) {
+    constexpr int VPL = F32 ? 4 : 8;
+    const int lane = threadIdx.x & 63;
+    const long long t = (long long)blockIdx.x * (ROUTER_THREADS / 64) + (threadIdx.x >> 6);
+    if (t >= a.T) return;
+    const size_t row = (size_t)t * a.E;
+    auto logit = [&](int e) __attribute__((always_inline)) {
+        const float x = F32 ? ((const float*)a.logits)[row + e] : (float)((const __bf16*)a.logits)[row + e];
+        return x != x ? -__builtin_inff() : x;
+    };
+    // lane j holds slot j (topk is at most the number of lanes)
+    int id = -1;
+    float G = 0.0f, l = -__builtin_inff();
+    if (lane < a.topk) {
+        id = a.ids_in[(size_t)t * a.topk + lane];
+        if ((unsigned)id < (unsigned)a.E) {
+            G = a.scale * a.d_gates[(size_t)t * a.topk + lane];
+            l = logit(id);
+        }
+        if (l == -__builtin_inff()) { id = -1; G = 0.0f; }                 // a masked expert has a weight of zero whatever its logit
+    }
+    const bool dense = a.score == MOE_ROUTER_SOFTMAX && !a.renormalise;
+    float top = -__builtin_inff(), all = 0.0f;
+    float first[VPL];                                                     // this lane's logits of the first step, kept for the second pass
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) first[i] = -__builtin_inff();
+    if (dense) {
+        // maximum and sum of the softmax in one pass over the row, then over the lanes
+        for (int e = lane * VPL; e < a.E; e += 64 * VPL) {
+            float v[VPL];
+            read_logits<F32, VPL, WIDE>(a.logits, row + e, e, a.E, v);
+            float m = top;
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) m = fmaxf(m, v[i]);
+            if (m != -__builtin_inff()) {
+                all *= top == -__builtin_inff() ? 0.0f : exp_below(top, m);
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) all += v[i] == -__builtin_inff() ? 0.0f : exp_below(v[i], m);
+                top = m;
+            }
+            if (e < 64 * VPL) {
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) first[i] = v[i];
+            }
+        }
+        const float m = key_value(moe::lanes_max<64>(order_key(top)));
+        all = moe::lanes_sum<64>(top == -__builtin_inff() ? 0.0f : all * exp_below(top, m));
+        top = m;
+    } else {
+        top = key_value(moe::lanes_max<64>(order_key(l)));
+    }
+    float w = 0.0f, slope = 1.0f;
+    if (id >= 0) {
+        if (a.score == MOE_ROUTER_SOFTMAX) w = exp_below(l, top);
+        else {
+            w = a.renormalise ? sigmoid_ratio(l, top) : sigmoid(l);
+            slope = sigmoid(-l);
+        }
+    }
+    if (a.renormalise) all = moe::lanes_sum<64>(w);
+    if (a.renormalise || dense) w = all > 0.0f ? w / all : 0.0f;
+    const float mean = moe::lanes_sum<64>(G * w);
+    // what slot j's expert gets beside the dense part
+    const float give = dense ? G : w * slope * (a.renormalise ? G - mean : G);
+    for (int e0 = 0; e0 < a.E; e0 += 64 * VPL) {                          // (by all lanes: each is asked for its slot)
+        const int e = e0 + lane * VPL;
+        float v[VPL], o[VPL];
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) o[i] = 0.0f;
+        for (int j = 0; j < a.topk; ++j) {
+            const int ej = __builtin_amdgcn_readlane(id, j);
+            const float gj = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, give), j));
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) o[i] += ej == e + i ? gj : 0.0f;
+        }
+        if (dense) {
+            if (e0 == 0) {
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) v[i] = first[i];
+            } else {
+                read_logits<F32, VPL, WIDE>(a.logits, row + e, e, a.E, v);
+            }
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) o[i] = v[i] == -__builtin_inff() ? 0.0f : exp_below(v[i], top) / all * (o[i] - mean);
+        }
+        if (e >= a.E) continue;
+        if constexpr (WIDE) {
+            if constexpr (F32) {
+                *reinterpret_cast<r_f32x4*>((float*)a.d_logits + row + e) = r_f32x4{o[0], o[1], o[2], o[3]};
+            } else {
+                typedef __attribute__((ext_vector_type(8))) __bf16 r_bf16x8;
+                r_bf16x8 b;
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) b[i] = (__bf16)o[i];
+                *reinterpret_cast<r_u32x4*>((__bf16*)a.d_logits + row + e) = __builtin_bit_cast(r_u32x4, b);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < VPL; ++i)
+                if (e + i < a.E) {
+                    if constexpr (F32) ((float*)a.d_logits)[row + e + i] = o[i];
+                    else ((__bf16*)a.d_logits)[row + e + i] = (__bf16)o[i];
+                }
+        }
+    }
+}
+
+template <bool F32, int LANES, int VPL> moe_status launch_topk(const RouterArgs& a, bool wide, hipStream_t s) {
+    constexpr int PER = ROUTER_THREADS / LANES;
+    moe::LaunchScope k("router_topk_kernel", s);
+    const dim3 grid((unsigned)((a.T - 1) / PER + 1)), block(ROUTER_THREADS);
+    if (wide) hipLaunchKernelGGL((router_topk_kernel<F32, LANES, VPL, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((router_topk_kernel<F32, LANES, VPL, false>), grid, block, 0, s, a);
+    return k.done();
+}
+template <bool F32> moe_status topk_of(const RouterArgs& a, bool wide, hipStream_t s) {
+    if (a.E <= 16) return launch_topk<F32, 16, 1>(a, wide, s);
+    if (a.E <= 64) return launch_topk<F32, 16, 4>(a, wide, s);
+    if (a.E <= 128) return launch_topk<F32, 16, 8>(a, wide, s);
+    if (a.E <= 256) return launch_topk<F32, 32, 8>(a, wide, s);
+    if (a.E <= 512) return launch_topk<F32, 64, 8>(a, wide, s);
+    if (a.E <= 1024) return launch_topk<F32, 64, 16>(a, wide, s);
+    return launch_topk<F32, 64, 64>(a, wide, s);
+}
+
+moe_status checked(int T, int E, int topk, int logits_type, int score, int flags, float scale) {
+    if (T < 0 || E < 1 || topk < 1 || topk > E) return MOE_ERR_INVALID_ARG;
+    if (logits_type != MOE_T_BF16 && logits_type != MOE_T_F32) return MOE_ERR_INVALID_ARG;
+    if ((score != MOE_ROUTER_SOFTMAX && score != MOE_ROUTER_SIGMOID) || (flags & ~MOE_ROUTER_RENORMALISE) || !(__builtin_fabsf(scale) < __builtin_inff())) return MOE_ERR_INVALID_ARG;
+    if (E > MOE_MAX_EXPERTS || topk > MOE_ROUTER_MAX_TOPK) return MOE_ERR_UNSUPPORTED_SHAPE;
+    return MOE_OK;
+}
+
+}  // namespace
+
+extern "C" moe_status moe_router_topk(const void* logits, int logits_type, int T, int E, int topk, int score, int flags, float scale, int32_t* ids, float* gates, void* hip_stream) {
+    if (const moe_status st = checked(T, E, topk, logits_type, score, flags, scale)) return st;
+    if (T == 0) return MOE_OK;
+    const bool f32 = logits_type == MOE_T_F32;
+    if (!logits || !ids || !gates || ((uintptr_t)logits & (f32 ? 3 : 1)) != 0 || (((uintptr_t)ids | (uintptr_t)gates) & 3) != 0) return MOE_ERR_INVALID_ARG;
+    const RouterArgs a = {logits, nullptr, nullptr, ids, gates, nullptr, scale, T, E, topk, score, flags & MOE_ROUTER_RENORMALISE};
+    // rows start on 16 bytes: pieces of 16 bytes, else one value at a time
+    const bool wide = ((uintptr_t)logits & 15) == 0 && E % (f32 ? 4 : 8) == 0;
+    return f32 ? topk_of<true>(a, wide, (hipStream_t)hip_stream) : topk_of<false>(a, wide, (hipStream_t)hip_stream);
+}
+
+extern "C" moe_status moe_router_topk_backward(const float* d_gates, const void* logits, int logits_type, const int32_t* ids, int T, int E, int topk, int score, int flags,
+                                               float scale, void* d_logits, void* hip_stream) {
+    if (const moe_status st = checked(T, E, topk, logits_type, score, flags, scale)) return st;
+    if (T == 0) return MOE_OK;
+    const bool f32 = logits_type == MOE_T_F32;
+    if (!d_gates || !logits || !ids || !d_logits || ((((uintptr_t)logits | (uintptr_t)d_logits) & (f32 ? 3 : 1)) != 0) || (((uintptr_t)ids | (uintptr_t)d_gates) & 3) != 0) return MOE_ERR_INVALID_ARG;
+    const RouterArgs a = {logits, ids, d_gates, nullptr, nullptr, d_logits, scale, T, E, topk, score, flags & MOE_ROUTER_RENORMALISE};
+    const bool wide = (((uintptr_t)logits | (uintptr_t)d_logits) & 15) == 0 && E % (f32 ? 4 : 8) == 0;
+    hipStream_t s = (hipStream_t)hip_stream;
+    const dim3 grid((unsigned)(((long long)T + 3) / 4)), block(ROUTER_THREADS);
+    moe::LaunchScope k("router_backward_kernel", s);
+    if (f32) {
+        if (wide) hipLaunchKernelGGL((router_backward_kernel<true, true>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((router_backward_kernel<true, false>), grid, block, 0, s, a);
+    } else {
+        if (wide) hipLaunchKernelGGL((router_backward_kernel<false, true>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((router_backward_kernel<false, false>), grid, block, 0, s, a);
+    }
+    return k.done();
+}
