@@ -410,7 +410,7 @@ moe_status moe_block_join_backward(const void* d_out, const void* d_next, const 
  *   y              out bf16 [M][d]; rows that no schedule row names are left untouched
  *   workspace          moe_ffn_w4_workspace_bytes(M, d, f) bytes, never less for a larger M
  * Limits: those of moe_expert_ffn_sliced, and M * max(d, f) * 2 < 2^32 - 256; finite scales below 2^116; x, y, the codes and the workspace
- * 16-byte aligned, scales 2-byte aligned.
+ * 16-byte aligned, scales and zero points 4-byte aligned.
  * ------------------------------------------------------------------------------------------- */
 size_t     moe_ffn_w4_workspace_bytes(int M, int d, int f);
 moe_status moe_expert_ffn_w4_sliced(const void* x, const int32_t* offsets, int M, int S, int E_loc, int d, int f, int group,

@@ -17,6 +17,7 @@
 #include "common.hpp"
 #include "rows.hpp"
 #include "parts.hpp"
+#include "plan.hpp"
 #include <type_traits>
 #include <algorithm>
 #include <cmath>
@@ -2483,6 +2484,22 @@ size_t bwd_part_bytes(int M, int d, int f) { return std::max(dw_places(M, d, f) 
 size_t bwd_workspace_bytes(int M, int E_loc, int d, int f) { return bwd_layout(M, E_loc, d, f).part + bwd_part_bytes(M, d, f); }
 
 }  // namespace
+
+namespace moe {
+size_t rows_plan_bytes(int M) { return plan_bytes(M) + ready_bytes(M) + 2 * list_bytes(M) + EBASE_BYTES; }
+moe_status rows_plan(RowsPlan& p, void* workspace, hipStream_t s) {
+    char* at = (char*)workspace;
+    auto take = [&](size_t bytes) { char* q = at; at += bytes; return q; };
+    p.blocks = (int4*)take(plan_bytes(p.M));
+    p.first = PLAN_HDR;
+    int* const ready = (int*)take(ready_bytes(p.M));
+    p.list = (int32_t*)take(list_bytes(p.M));
+    float* const gate = (float*)take(list_bytes(p.M));
+    p.gate = p.row_gate ? gate : nullptr;
+    const PlanArgs a = {p.offsets, p.S, p.e_loc, p.M, p.block_rows, plan_capacity(p.M), p.blocks, ready, p.row_map, p.row_gate, p.list, p.gate, (int*)take(EBASE_BYTES), nullptr};
+    return launch_plan(a, s);
+}
+}  // namespace moe
 
 extern "C" size_t moe_ffn_workspace_bytes(int M, int d, int f) {
     if (M < 0 || d < 1 || f < 1) return 0;

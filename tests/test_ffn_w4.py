@@ -106,7 +106,7 @@ def test_refusals_need_no_gpu(hostlib):
         assert f(**{name: None}) == -1, name
     for name in ("x", "y", "qg", "qu", "qd", "ws"):
         assert f(**{name: odd}) == -1, name
-    for name in ("sg", "su", "sd", "rm", "rg", "off"):
+    for name in ("sg", "su", "sd", "zg", "zu", "zd", "rm", "rg", "off"):
         assert f(**{name: one}) == -1, name
     for G in (0, 16, 48, 256, -32):
         assert f(G=G) == -2
