@@ -454,31 +454,32 @@ def moe_combine_topk_sum(y, row_of, gate=None, out=None):
 
 # --------------------------------------------------------------------------------------------- around the experts
 def _operands(what, wanted):
-    """wanted: (name, tensor or None, dtype or allowed dtypes, shape).  All tensors contiguous, of that type and shape, on one device, which is
-    made current for the call; returns the context that does so and the handle of the device's stream."""
-    import torch
-    device = None
+    """wanted: (name, tensor or None, dtype or allowed dtypes, shape).  All tensors contiguous, of that type and shape, and on one GPU, whose number is
+    returned."""
+    device = -1
     for name, t, dtype, shape in wanted:
         if t is None:
             continue
-        if not t.is_cuda or not t.is_contiguous() or (t.dtype not in dtype if isinstance(dtype, tuple) else t.dtype != dtype) or tuple(t.shape) != shape:
+        at = t.get_device()
+        if at < 0 or t.shape != shape or not t.is_contiguous() or (t.dtype is not dtype and (type(dtype) is not tuple or t.dtype not in dtype)):
             raise MoeError("%s: %s must be a contiguous CUDA tensor of dtype %s and shape %s" % (what, name, dtype, list(shape)))
-        if device is None:
-            device = t.get_device()
-        elif t.get_device() != device:
-            raise MoeError("%s: %s is on another device" % (what, name))
+        if at != device:
+            if device >= 0:
+                raise MoeError("%s: %s is on another device" % (what, name))
+            device = at
     return device
 
 
-def _on(device, what, call):
-    """call(stream handle) on the current stream of `device`."""
+def _on(device, what, call, *args):
+    """call(*args, stream) on the current stream of `device`, which is made current for it."""
     import torch
-    if device != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            rc = call(torch.cuda.current_stream(device).cuda_stream)
+    if device == torch.cuda.current_device():
+        rc = call(*args, torch._C._cuda_getCurrentRawStream(device))
     else:
-        rc = call(torch.cuda.current_stream(device).cuda_stream)
-    _check(rc, what)
+        with torch.cuda.device(device):
+            rc = call(*args, torch._C._cuda_getCurrentRawStream(device))
+    if rc:
+        _check(rc, what)
 
 
 def _two(t, what, name):
@@ -508,7 +509,7 @@ def moe_block_norm(x, weight, eps: float = 1e-6, out=None):
     if out is None:
         out = torch.empty((T, d), dtype=torch.bfloat16, device=x.device)
     dev = _operands(what, (("x", x, (torch.bfloat16, torch.float32), (T, d)), ("weight", weight, torch.float32, (d,)), ("out", out, torch.bfloat16, (T, d))))
-    _on(dev, what, lambda s: load().moe_block_norm(x.data_ptr(), int(x.dtype == torch.float32), _at(weight), eps, T, d, out.data_ptr(), s))
+    _on(dev, what, load().moe_block_norm, x.data_ptr(), int(x.dtype == torch.float32), _at(weight), eps, T, d, out.data_ptr())
     return out
 
 
@@ -521,8 +522,8 @@ def moe_block_norm_backward(d_out, x, weight, eps: float = 1e-6, d_stream=None, 
                            ("d_stream", d_stream, x.dtype, (T, d))))
     o = dict(d_x=torch.empty_like(x), d_weight=torch.empty_like(weight))
     workspace = _bytes(int(load().moe_block_backward_workspace_bytes(T, d)), workspace, x, what)
-    _on(dev, what, lambda s: load().moe_block_norm_backward(_at(d_out), x.data_ptr(), int(x.dtype == torch.float32), _at(weight), _at(d_stream), eps, T, d,
-                                                            o["d_x"].data_ptr(), o["d_weight"].data_ptr(), workspace.data_ptr(), workspace.numel(), s))
+    _on(dev, what, load().moe_block_norm_backward, _at(d_out), x.data_ptr(), int(x.dtype == torch.float32), _at(weight), _at(d_stream), eps, T, d,
+        o["d_x"].data_ptr(), o["d_weight"].data_ptr(), workspace.data_ptr(), workspace.numel())
     return o
 
 
@@ -532,6 +533,7 @@ def moe_block_join(z, stream, post_weight=None, gate=None, next_weight=None, sca
     import torch
     what = "moe_block_join"
     T, d = _two(z, what, "z")
+    _two(stream, what, "stream")
     if out is None:
         out = torch.empty_like(stream)
     if next_out is None and next_weight is not None:
@@ -540,8 +542,8 @@ def moe_block_join(z, stream, post_weight=None, gate=None, next_weight=None, sca
     dev = _operands(what, (("z", z, torch.bfloat16, (T, d)), ("stream", stream, stream_types, (T, d)), ("post_weight", post_weight, torch.float32, (d,)),
                            ("gate", gate, torch.float32, (T,)), ("next_weight", next_weight, torch.float32, (d,)), ("out", out, stream.dtype, (T, d)),
                            ("next_out", next_out, torch.bfloat16, (T, d))))
-    _on(dev, what, lambda s: load().moe_block_join(z.data_ptr(), stream.data_ptr(), int(stream.dtype == torch.float32), _at(post_weight), _at(gate), _at(next_weight),
-                                                   scale, eps, T, d, out.data_ptr(), _at(next_out), s))
+    _on(dev, what, load().moe_block_join, z.data_ptr(), stream.data_ptr(), int(stream.dtype == torch.float32), _at(post_weight), _at(gate),
+        _at(next_weight), scale, eps, T, d, out.data_ptr(), _at(next_out))
     return out, next_out
 
 
@@ -561,10 +563,9 @@ def moe_block_join_backward(d_out, d_next, z, out, post_weight=None, gate=None, 
     like = lambda t: None if t is None else torch.empty_like(t)                              # noqa: E731
     o = dict(d_z=torch.empty_like(z), d_stream=torch.empty_like(out), d_gate=like(gate), d_post_weight=like(post_weight), d_next_weight=like(next_weight))
     workspace = _bytes(int(load().moe_block_backward_workspace_bytes(T, d)), workspace, z, what)
-    _on(dev, what, lambda s: load().moe_block_join_backward(_at(d_out), _at(d_next), z.data_ptr(), out.data_ptr(), int(out.dtype == torch.float32), _at(post_weight),
-                                                            _at(gate), _at(next_weight), scale, eps, T, d, o["d_z"].data_ptr(), o["d_stream"].data_ptr(),
-                                                            _at(o["d_gate"]), _at(o["d_post_weight"]), _at(o["d_next_weight"]), workspace.data_ptr(),
-                                                            workspace.numel(), s))
+    _on(dev, what, load().moe_block_join_backward, _at(d_out), _at(d_next), z.data_ptr(), out.data_ptr(), int(out.dtype == torch.float32),
+        _at(post_weight), _at(gate), _at(next_weight), scale, eps, T, d, o["d_z"].data_ptr(), o["d_stream"].data_ptr(), _at(o["d_gate"]),
+        _at(o["d_post_weight"]), _at(o["d_next_weight"]), workspace.data_ptr(), workspace.numel())
     return o
 
 
@@ -588,8 +589,8 @@ def moe_router_topk(logits, topk: int, score: str = "softmax", renormalise: bool
         gates = torch.empty((T, topk), dtype=torch.float32, device=logits.device)
     dev = _operands(what, (("logits", logits, (torch.bfloat16, torch.float32), (T, E)), ("ids", ids, torch.int32, (T, topk)), ("gates", gates, torch.float32, (T, topk))))
     sc = _score(score, what)
-    _on(dev, what, lambda s: load().moe_router_topk(logits.data_ptr(), int(logits.dtype == torch.float32), T, E, topk, sc, MOE_ROUTER_RENORMALISE if renormalise else 0,
-                                                    scale, ids.data_ptr(), gates.data_ptr(), s))
+    _on(dev, what, load().moe_router_topk, logits.data_ptr(), int(logits.dtype == torch.float32), T, E, topk, sc,
+        MOE_ROUTER_RENORMALISE if renormalise else 0, scale, ids.data_ptr(), gates.data_ptr())
     return ids, gates
 
 
@@ -604,8 +605,8 @@ def moe_router_topk_backward(d_gates, logits, ids, score: str = "softmax", renor
     dev = _operands(what, (("d_gates", d_gates, torch.float32, (T, topk)), ("logits", logits, (torch.bfloat16, torch.float32), (T, E)), ("ids", ids, torch.int32, (T, topk)),
                            ("d_logits", d_logits, logits.dtype, (T, E))))
     sc = _score(score, what)
-    _on(dev, what, lambda s: load().moe_router_topk_backward(d_gates.data_ptr(), logits.data_ptr(), int(logits.dtype == torch.float32), ids.data_ptr(), T, E, topk, sc,
-                                                             MOE_ROUTER_RENORMALISE if renormalise else 0, scale, d_logits.data_ptr(), s))
+    _on(dev, what, load().moe_router_topk_backward, d_gates.data_ptr(), logits.data_ptr(), int(logits.dtype == torch.float32), ids.data_ptr(), T,
+        E, topk, sc, MOE_ROUTER_RENORMALISE if renormalise else 0, scale, d_logits.data_ptr())
     return d_logits
 
 
@@ -619,8 +620,8 @@ def moe_combine_topk_sum_backward(d_out, y, row_of, gate=None, workspace=None):
                            ("gate", gate, torch.float32, (T, topk))))
     o = dict(d_y=torch.empty_like(y), d_gate=None if gate is None else torch.empty_like(gate))
     workspace = _bytes(int(load().moe_combine_backward_workspace_bytes(R)), workspace, y, what)
-    _on(dev, what, lambda s: load().moe_combine_topk_sum_backward(_at(d_out), y.data_ptr(), row_of.data_ptr(), _at(gate), T, topk, d, R, o["d_y"].data_ptr(),
-                                                                  _at(o["d_gate"]), workspace.data_ptr(), workspace.numel(), s))
+    _on(dev, what, load().moe_combine_topk_sum_backward, _at(d_out), y.data_ptr(), row_of.data_ptr(), _at(gate), T, topk, d, R,
+        o["d_y"].data_ptr(), _at(o["d_gate"]), workspace.data_ptr(), workspace.numel())
     return o
 
 
@@ -652,9 +653,9 @@ def moe_expert_ffn_w4_sliced(x, offsets, S: int, E_loc: int, q_gate, q_up, q_dow
                            ("s_down", s_down, torch.bfloat16, down), ("z_gate", z_gate, torch.uint8, up), ("z_up", z_up, torch.uint8, up),
                            ("z_down", z_down, torch.uint8, down), ("row_map", row_map, torch.int32, (M,)), ("row_gate", row_gate, torch.float32, (M,))))
     workspace = _bytes(moe_ffn_w4_workspace_bytes(M, d, f), workspace, x, what)
-    _on(dev, what, lambda s: load().moe_expert_ffn_w4_sliced(
-        x.data_ptr(), offsets.data_ptr(), M, S, E_loc, d, f, group, q_gate.data_ptr(), q_up.data_ptr(), q_down.data_ptr(), s_gate.data_ptr(), s_up.data_ptr(),
-        s_down.data_ptr(), _at(z_gate), _at(z_up), _at(z_down), _at(row_map), _at(row_gate), y.data_ptr(), workspace.data_ptr(), workspace.numel(), s))
+    _on(dev, what, load().moe_expert_ffn_w4_sliced, x.data_ptr(), offsets.data_ptr(), M, S, E_loc, d, f, group, q_gate.data_ptr(), q_up.data_ptr(),
+        q_down.data_ptr(), s_gate.data_ptr(), s_up.data_ptr(), s_down.data_ptr(), _at(z_gate), _at(z_up), _at(z_down), _at(row_map), _at(row_gate),
+        y.data_ptr(), workspace.data_ptr(), workspace.numel())
     return y
 
 

@@ -160,7 +160,7 @@ struct BackwardArgs {
 // Three sums over the columns of a row meet in one reduction (out^2, d_next w2 out, z^2), the fourth (D w1 z) in a second one.
 // The sums over the tokens stay in registers while a workgroup walks its rows.
 template <int NT, int NV, bool F32, bool JOIN>
-__global__ __launch_bounds__(NT == 64 ? 256 : NT)
+__global__ __attribute__((amdgpu_waves_per_eu(4))) __launch_bounds__(NT == 64 ? 256 : NT)
 void block_backward_kernel(BackwardArgs a) {
     constexpr int PER = NT == 64 ? 4 : 1;
     __shared__ float s_sum3[2 * 3 * (NT / 64)], s_sum1[2 * (NT / 64)];
@@ -347,7 +347,7 @@ template <int NT, int NV, bool F32, bool JOIN> moe_status backward(BackwardArgs 
 template <bool F32, bool JOIN> moe_status backward_of(const BackwardArgs& a, float* d_w1, float* d_w2, float* work, hipStream_t s) {
     if (a.d <= 512) return backward<64, 1, F32, JOIN>(a, d_w1, d_w2, work, s);
     if (a.d <= 1024) return backward<64, 2, F32, JOIN>(a, d_w1, d_w2, work, s);
-    if (a.d <= 2048) return backward<128, 2, F32, JOIN>(a, d_w1, d_w2, work, s);
+    if (a.d <= 2048) return backward<256, 1, F32, JOIN>(a, d_w1, d_w2, work, s);
     if (a.d <= 4096) return backward<256, 2, F32, JOIN>(a, d_w1, d_w2, work, s);
     if (a.d <= 8192) return backward<512, 2, F32, JOIN>(a, d_w1, d_w2, work, s);
     return backward<1024, 2, F32, JOIN>(a, d_w1, d_w2, work, s);

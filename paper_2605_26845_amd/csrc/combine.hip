@@ -125,7 +125,7 @@ extern "C" moe_status moe_combine_topk_sum(const void* y, const int32_t* row_of,
 // moe_combine_topk_sum_backward: d_y[row_of[t][j]] += gate[t][j] d_out[t], d_gate[t][j] = d_out[t] . y[row_of[t][j]].
 // HBM bound: d_out is read once, y read and d_y written once.  A workgroup takes a token: its threads hold d_out[t] (8 columns a
 // step) and walk the token's rows, whose loads go out together.  Nearly always a row belongs to one assignment and is written right here.  A row that
-// several assignments name (counted beforehand) is left to combine_backward_rest_kernel, which adds them up in the order of the assignments, and so
+// several assignments name (counted beforehand) is left to the workgroups behind the tokens', which add them up in the order of the assignments, and so
 // is a row that none names, whose gradient is zero.
 namespace {
 
@@ -142,6 +142,21 @@ void combine_count_kernel(const int32_t* __restrict__ row_of, int n, int R, int3
         const int r = row_of[i];
         if ((unsigned)r < (unsigned)R) atomicAdd(uses + r, 1);
     }
+}
+
+// both for few rows and assignments, in LDS: one launch instead of two
+constexpr int COUNT_ROWS = 16384;
+__global__ __launch_bounds__(1024)
+void combine_count_few_kernel(const int32_t* __restrict__ row_of, int n, int R, int32_t* __restrict__ uses) {
+    __shared__ int32_t s_uses[COUNT_ROWS];
+    for (int r = threadIdx.x; r < R; r += 1024) s_uses[r] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += 1024) {
+        const int r = row_of[i];
+        if ((unsigned)r < (unsigned)R) atomicAdd(s_uses + r, 1);
+    }
+    __syncthreads();
+    for (int r = threadIdx.x; r < R; r += 1024) uses[r] = s_uses[r];
 }
 
 struct CombineBackwardArgs {
@@ -166,6 +181,62 @@ __device__ __forceinline__ cb_u32x4 cb_scaled(const float (&v)[8], float w) {
     return __builtin_bit_cast(cb_u32x4, o);
 }
 
+// Rows that no assignment names, or several do, by workgroup `first` of `step`, which looks at a row per thread; the several are found by going through
+// all assignments, a workgroup's width at a time, and added in their order.
+template <int THREADS>
+__device__ __forceinline__ void combine_backward_rest(const CombineBackwardArgs& a, int first, int step) {
+    constexpr int W = THREADS / 64;
+    __shared__ unsigned long long s_hit[W], s_odd[W];
+    const int wave = threadIdx.x >> 6;
+    const long long n = (long long)a.T * a.topk;
+    for (long long r0 = (long long)first * THREADS; r0 < a.R; r0 += (long long)step * THREADS) {
+        const unsigned long long odd = __ballot(r0 + threadIdx.x < a.R && a.uses[r0 + threadIdx.x] != 1);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) s_odd[wave] = odd;
+        __syncthreads();
+        for (int q = 0; q < THREADS; ++q) {
+            if (s_odd[q >> 6] == 0) { q |= 63; continue; }
+            if (!((s_odd[q >> 6] >> (q & 63)) & 1)) continue;
+            const long long r = r0 + q;
+            const int uses = a.uses[r];                                        // (the same for the whole workgroup)
+            if (uses == 0) {
+                for (int col = threadIdx.x * 8; col < a.d; col += THREADS * 8) *reinterpret_cast<cb_u32x4*>(a.d_y + (size_t)r * a.d + col) = cb_u32x4{0u, 0u, 0u, 0u};
+                continue;
+            }
+            for (int c0 = 0; c0 < a.d; c0 += THREADS * 8) {
+                const int col = c0 + threadIdx.x * 8;
+                float sum[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) sum[c] = 0.0f;
+                int left = uses;
+                for (long long i0 = 0; i0 < n && left > 0; i0 += THREADS) {
+                    const long long i = i0 + threadIdx.x;
+                    const unsigned long long hit = __ballot(i < n && a.row_of[i < n ? i : 0] == r);
+                    if ((threadIdx.x & 63) == 0) s_hit[wave] = hit;
+                    __syncthreads();
+                    for (int w = 0; w < W; ++w) {
+                        unsigned long long h = s_hit[w];
+                        while (h) {
+                            const int at = (int)i0 + w * 64 + __builtin_ctzll(h);
+                            h &= h - 1;
+                            --left;
+                            if (col < a.d) {
+                                const float g = a.gate ? a.gate[at] : 1.0f;
+                                float v[8];
+                                cb_widen(*reinterpret_cast<const cb_u32x4*>(a.d_out + (size_t)(at / a.topk) * a.d + col), v);
+#pragma unroll
+                                for (int c = 0; c < 8; ++c) sum[c] = __builtin_fmaf(g, v[c], sum[c]);
+                            }
+                        }
+                    }
+                    __syncthreads();
+                }
+                if (col < a.d) *reinterpret_cast<cb_u32x4*>(a.d_y + (size_t)r * a.d + col) = cb_scaled(sum, 1.0f);
+            }
+        }
+    }
+}
+
 // NT threads per token, NV steps of NT * 8 columns, J rows of y in flight at once
 template <int NT, int NV, int J>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT)
@@ -174,6 +245,11 @@ void combine_backward_kernel(CombineBackwardArgs a) {
     __shared__ float s_sum[2 * J * (NT / 64)];
     int half = 0;
     const int tid = threadIdx.x % NT;
+    const int token_blocks = a.T == 0 ? 0 : (a.T - 1) / PER + 1;
+    if ((int)blockIdx.x >= token_blocks) {                                // the workgroups behind the tokens'
+        combine_backward_rest<(NT == 64 ? 256 : NT)>(a, (int)blockIdx.x - token_blocks, (int)gridDim.x - token_blocks);
+        return;
+    }
     const long long t = (long long)blockIdx.x * PER + (int)threadIdx.x / NT;
     if (t >= a.T) return;                                                 // (a whole wavefront, which meets no barrier if NT is 64)
     cb_u32x4 raw[NV];
@@ -230,54 +306,10 @@ void combine_backward_kernel(CombineBackwardArgs a) {
     }
 }
 
-// rows that no assignment names, or several do: those are found by going through all assignments, 256 at a time, and added in their order
-__global__ __launch_bounds__(256)
-void combine_backward_rest_kernel(CombineBackwardArgs a) {
-    __shared__ unsigned long long s_hit[4];
-    const int wave = threadIdx.x >> 6, n = a.T * a.topk;
-    for (long long r = blockIdx.x; r < a.R; r += gridDim.x) {
-        const int uses = a.uses[r];                                        // (the same for the whole workgroup)
-        if (uses == 1) continue;
-        if (uses == 0) {
-            for (int col = threadIdx.x * 8; col < a.d; col += 256 * 8) *reinterpret_cast<cb_u32x4*>(a.d_y + (size_t)r * a.d + col) = cb_u32x4{0u, 0u, 0u, 0u};
-            continue;
-        }
-        for (int c0 = 0; c0 < a.d; c0 += 256 * 8) {
-            const int col = c0 + threadIdx.x * 8;
-            float sum[8];
-#pragma unroll
-            for (int c = 0; c < 8; ++c) sum[c] = 0.0f;
-            int left = uses;
-            for (long long i0 = 0; i0 < n && left > 0; i0 += 256) {
-                const long long i = i0 + threadIdx.x;
-                const unsigned long long hit = __ballot(i < n && a.row_of[i < n ? i : 0] == r);
-                if ((threadIdx.x & 63) == 0) s_hit[wave] = hit;
-                __syncthreads();
-                for (int w = 0; w < 4; ++w) {
-                    unsigned long long h = s_hit[w];
-                    while (h) {
-                        const int at = (int)i0 + w * 64 + __builtin_ctzll(h);
-                        h &= h - 1;
-                        --left;
-                        if (col < a.d) {
-                            const float g = a.gate ? a.gate[at] : 1.0f;
-                            float v[8];
-                            cb_widen(*reinterpret_cast<const cb_u32x4*>(a.d_out + (size_t)(at / a.topk) * a.d + col), v);
-#pragma unroll
-                            for (int c = 0; c < 8; ++c) sum[c] = __builtin_fmaf(g, v[c], sum[c]);
-                        }
-                    }
-                }
-                __syncthreads();
-            }
-            if (col < a.d) *reinterpret_cast<cb_u32x4*>(a.d_y + (size_t)r * a.d + col) = cb_scaled(sum, 1.0f);
-        }
-    }
-}
-
 template <int NT, int NV, int J> void launch_combine_backward(const CombineBackwardArgs& a, hipStream_t s) {
     constexpr int PER = NT == 64 ? 4 : 1;
-    hipLaunchKernelGGL((combine_backward_kernel<NT, NV, J>), dim3((unsigned)((a.T - 1) / PER + 1)), dim3(NT == 64 ? 256 : NT), 0, s, a);
+    const int token_blocks = a.T == 0 ? 0 : (a.T - 1) / PER + 1, rest_blocks = a.R == 0 ? 0 : std::min((a.R - 1) / (NT == 64 ? 256 : NT) + 1, moe::compute_units());
+    hipLaunchKernelGGL((combine_backward_kernel<NT, NV, J>), dim3((unsigned)token_blocks + (unsigned)rest_blocks), dim3(NT == 64 ? 256 : NT), 0, s, a);
 }
 template <int NT, int NV> void launch_combine_backward(const CombineBackwardArgs& a, hipStream_t s) {
     if (a.topk == 1) launch_combine_backward<NT, NV, 1>(a, s);
@@ -302,11 +334,15 @@ extern "C" moe_status moe_combine_topk_sum_backward(const void* d_out, const voi
     const auto blocks = [&](int items) { return dim3((unsigned)std::min((items - 1) / 256 + 1, cus * 8)); };
     if (R > 0) {
         moe::LaunchScope k("combine_count_kernel", s);
-        hipLaunchKernelGGL(combine_clear_kernel, blocks(R), dim3(256), 0, s, (int32_t*)workspace, R);
-        if (n > 0) hipLaunchKernelGGL(combine_count_kernel, blocks(n), dim3(256), 0, s, row_of, n, R, (int32_t*)workspace);
+        if (R <= COUNT_ROWS && n <= COUNT_ROWS) {
+            hipLaunchKernelGGL(combine_count_few_kernel, dim3(1), dim3(1024), 0, s, row_of, n, R, (int32_t*)workspace);
+        } else {
+            hipLaunchKernelGGL(combine_clear_kernel, blocks(R), dim3(256), 0, s, (int32_t*)workspace, R);
+            if (n > 0) hipLaunchKernelGGL(combine_count_kernel, blocks(n), dim3(256), 0, s, row_of, n, R, (int32_t*)workspace);
+        }
         if (const moe_status st = k.done()) return st;
     }
-    if (T > 0) {
+    if (T > 0 || R > 0) {
         moe::LaunchScope k("combine_backward_kernel", s);
         if (d <= 512) launch_combine_backward<64, 1>(a, s);
         else if (d <= 1024) launch_combine_backward<64, 2>(a, s);
@@ -314,11 +350,6 @@ extern "C" moe_status moe_combine_topk_sum_backward(const void* d_out, const voi
         else if (d <= 4096) launch_combine_backward<256, 2>(a, s);
         else if (d <= 8192) launch_combine_backward<512, 2>(a, s);
         else launch_combine_backward<1024, 2>(a, s);
-        if (const moe_status st = k.done()) return st;
-    }
-    if (R > 0) {
-        moe::LaunchScope k("combine_backward_rest_kernel", s);
-        hipLaunchKernelGGL(combine_backward_rest_kernel, dim3((unsigned)std::min(R, cus * 8)), dim3(256), 0, s, a);
         if (const moe_status st = k.done()) return st;
     }
     return MOE_OK;

@@ -180,107 +180,139 @@ void router_topk_kernel(RouterArgs a) {
     }
 }
 
-// One wavefront per token; a lane writes VPL neighbouring logits' gradients at a time.  With G_j = scale d_gate_j over the slots whose expert is in range:
+// exp(x) for x <= 0 to 2 steps: x log2(e) in two parts, the hardware's power of two of the first, the second to first order (below 2^-126: zero)
+__device__ __forceinline__ float exp_negative(float x) {
+    const float y = fmaxf(x, -200.0f), t = y * 1.44269504f;
+    const float r = __builtin_fmaf(y, 1.44269504f, -t) + y * 1.9259629e-8f, e = __builtin_amdgcn_exp2f(t);
+    return __builtin_fmaf(e, r * 0.693147182f, e);
+}
+__device__ __forceinline__ float exp_below_fast(float x, float top) { return x == top ? 1.0f : exp_negative(x - top); }
+
+// LANES lanes per token (topk of them at least), which go through its experts in steps of LANES * VPL.  With G_j = scale d_gate_j over the slots whose expert is in range:
 //   softmax                 d_l[e] = p_e (sum of G_j with id_j = e  -  sum_j G_j p_j)
 //   renormalised (w_j sum to one over the slots)      d_l[id_j] += w_j (1 - sigmoid(l_j) for sigmoid scores, else 1) (G_j - sum_k G_k w_k)
 //   sigmoid                 d_l[id_j] += G_j s_j (1 - s_j)
-template <bool F32, bool WIDE>
+// What a slot gives its expert meets the expert's lane in LDS, a row of E floats per token.  Bound by the vector instructions of the exponentials: each is taken once
+// (16384 tokens of 256 experts: with a second one per logit, a wavefront per token and every lane asking every slot 16.5 us).
+template <bool F32, int LANES, int VPL, bool WIDE>
 __global__ __launch_bounds__(ROUTER_THREADS)
 void router_backward_kernel(RouterArgs a) {
-    constexpr int VPL = F32 ? 4 : 8;
-    const int lane = threadIdx.x & 63;
-    const long long t = (long long)blockIdx.x * (ROUTER_THREADS / 64) + (threadIdx.x >> 6);
-    if (t >= a.T) return;
-    const size_t row = (size_t)t * a.E;
-    auto logit = [&](int e) __attribute__((always_inline)) {
-        const float x = F32 ? ((const float*)a.logits)[row + e] : (float)((const __bf16*)a.logits)[row + e];
-        return x != x ? -__builtin_inff() : x;
-    };
-    // lane j holds slot j (topk is at most the number of lanes)
+    extern __shared__ __attribute__((aligned(16))) float s_give[];
+    const int sub = threadIdx.x % LANES;
+    const long long t = (long long)blockIdx.x * (ROUTER_THREADS / LANES) + threadIdx.x / LANES;
+    const bool live = t < a.T;                                             // (lanes of other tokens take part in the wavefront's exchanges)
+    const size_t row = live ? (size_t)t * a.E : 0;
+    const int pitch = (a.E + 3) & ~3;                                      // (16 bytes)
+    float* const give_row = s_give + (threadIdx.x / LANES) * pitch;
+    for (int e = sub * 4; e < a.E; e += LANES * 4) *reinterpret_cast<r_f32x4*>(give_row + e) = r_f32x4{0.f, 0.f, 0.f, 0.f};
+    // lane j holds slot j
     int id = -1;
     float G = 0.0f, l = -__builtin_inff();
-    if (lane < a.topk) {
-        id = a.ids_in[(size_t)t * a.topk + lane];
+    if (live && sub < a.topk) {
+        id = a.ids_in[(size_t)t * a.topk + sub];
         if ((unsigned)id < (unsigned)a.E) {
-            G = a.scale * a.d_gates[(size_t)t * a.topk + lane];
-            l = logit(id);
+            G = a.scale * a.d_gates[(size_t)t * a.topk + sub];
+            l = F32 ? ((const float*)a.logits)[row + id] : (float)((const __bf16*)a.logits)[row + id];
         }
-        if (l == -__builtin_inff()) { id = -1; G = 0.0f; }                 // a masked expert has a weight of zero whatever its logit
+        if (!(l > -__builtin_inff())) { id = -1; G = 0.0f; l = -__builtin_inff(); }      // a masked expert has a weight of zero whatever its logit
     }
     const bool dense = a.score == MOE_ROUTER_SOFTMAX && !a.renormalise;
     float top = -__builtin_inff(), all = 0.0f;
-    float first[VPL];                                                     // this lane's logits of the first step, kept for the second pass
+    float first[VPL], first_top = -__builtin_inff();                      // this lane's exponentials of the first step, over its own largest
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) first[i] = -__builtin_inff();
-    if (dense) {
+    for (int i = 0; i < VPL; ++i) first[i] = 0.0f;
+    if (dense && live) {
         // maximum and sum of the softmax in one pass over the row, then over the lanes
-        for (int e = lane * VPL; e < a.E; e += 64 * VPL) {
+        for (int e = sub * VPL; e < a.E; e += LANES * VPL) {
             float v[VPL];
             read_logits<F32, VPL, WIDE>(a.logits, row + e, e, a.E, v);
             float m = top;
 #pragma unroll
             for (int i = 0; i < VPL; ++i) m = fmaxf(m, v[i]);
             if (m != -__builtin_inff()) {
-                all *= top == -__builtin_inff() ? 0.0f : exp_below(top, m);
+                all *= top == -__builtin_inff() ? 0.0f : exp_below_fast(top, m);
 #pragma unroll
-                for (int i = 0; i < VPL; ++i) all += v[i] == -__builtin_inff() ? 0.0f : exp_below(v[i], m);
+                for (int i = 0; i < VPL; ++i) {
+                    v[i] = v[i] == -__builtin_inff() ? 0.0f : exp_below_fast(v[i], m);
+                    all += v[i];
+                }
                 top = m;
+            } else {
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) v[i] = 0.0f;
             }
-            if (e < 64 * VPL) {
+            if (e < LANES * VPL) {
+                first_top = top;
 #pragma unroll
                 for (int i = 0; i < VPL; ++i) first[i] = v[i];
             }
         }
-        const float m = key_value(moe::lanes_max<64>(order_key(top)));
-        all = moe::lanes_sum<64>(top == -__builtin_inff() ? 0.0f : all * exp_below(top, m));
-        top = m;
-    } else {
-        top = key_value(moe::lanes_max<64>(order_key(l)));
     }
+    const float mine = dense ? top : l;
+    const float most = key_value(moe::lanes_max<LANES>(order_key(mine)));
+    if (dense) all = moe::lanes_sum<LANES>(top == -__builtin_inff() ? 0.0f : all * exp_below_fast(top, most));
+    top = most;
     float w = 0.0f, slope = 1.0f;
     if (id >= 0) {
-        if (a.score == MOE_ROUTER_SOFTMAX) w = exp_below(l, top);
+        if (a.score == MOE_ROUTER_SOFTMAX) w = exp_below_fast(l, top);
         else {
             w = a.renormalise ? sigmoid_ratio(l, top) : sigmoid(l);
             slope = sigmoid(-l);
         }
     }
-    if (a.renormalise) all = moe::lanes_sum<64>(w);
+    if (a.renormalise) all = moe::lanes_sum<LANES>(w);
     if (a.renormalise || dense) w = all > 0.0f ? w / all : 0.0f;
-    const float mean = moe::lanes_sum<64>(G * w);
+    const float mean = moe::lanes_sum<LANES>(G * w);
     // what slot j's expert gets beside the dense part
     const float give = dense ? G : w * slope * (a.renormalise ? G - mean : G);
-    for (int e0 = 0; e0 < a.E; e0 += 64 * VPL) {                          // (by all lanes: each is asked for its slot)
-        const int e = e0 + lane * VPL;
-        float v[VPL], o[VPL];
-#pragma unroll
-        for (int i = 0; i < VPL; ++i) o[i] = 0.0f;
+    // Each slot puts its number at its expert's place; who finds another one there shares the expert, and then the slots add theirs one after the other.
+    // (One wavefront's LDS accesses are in order; the compiler must not know better.)
+    asm volatile("" ::: "memory");
+    if (id >= 0) give_row[id] = __builtin_bit_cast(float, 0x7F800001 + sub);
+    asm volatile("" ::: "memory");
+    const bool shared = id >= 0 && __builtin_bit_cast(int, give_row[id]) != 0x7F800001 + sub;
+    asm volatile("" ::: "memory");
+    if (__ballot(shared) == 0ull) {
+        if (id >= 0) give_row[id] = give;
+    } else {
+        if (id >= 0) give_row[id] = 0.0f;
         for (int j = 0; j < a.topk; ++j) {
-            const int ej = __builtin_amdgcn_readlane(id, j);
-            const float gj = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, give), j));
-#pragma unroll
-            for (int i = 0; i < VPL; ++i) o[i] += ej == e + i ? gj : 0.0f;
+            asm volatile("" ::: "memory");
+            if (id >= 0 && sub == j) give_row[id] += give;
         }
+    }
+    asm volatile("" ::: "memory");
+    const float by = all > 0.0f ? exp_below_fast(first_top, top) / all : 0.0f;
+    if (!live) return;
+    for (int e = sub * VPL; e < a.E; e += LANES * VPL) {
+        float o[VPL];
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) o[i] = e + i < a.E ? give_row[e + i] : 0.0f;
         if (dense) {
-            if (e0 == 0) {
+            if (e < LANES * VPL) {
 #pragma unroll
-                for (int i = 0; i < VPL; ++i) v[i] = first[i];
+                for (int i = 0; i < VPL; ++i) o[i] = first[i] * by * (o[i] - mean);
             } else {
+                float v[VPL];
                 read_logits<F32, VPL, WIDE>(a.logits, row + e, e, a.E, v);
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) o[i] = v[i] == -__builtin_inff() ? 0.0f : exp_below_fast(v[i], top) / all * (o[i] - mean);
             }
-#pragma unroll
-            for (int i = 0; i < VPL; ++i) o[i] = v[i] == -__builtin_inff() ? 0.0f : exp_below(v[i], top) / all * (o[i] - mean);
         }
-        if (e >= a.E) continue;
-        if constexpr (WIDE) {
-            if constexpr (F32) {
-                *reinterpret_cast<r_f32x4*>((float*)a.d_logits + row + e) = r_f32x4{o[0], o[1], o[2], o[3]};
-            } else {
-                typedef __attribute__((ext_vector_type(8))) __bf16 r_bf16x8;
-                r_bf16x8 b;
+        constexpr int PIECE = F32 ? 4 : 8;
+        if constexpr (WIDE && VPL % PIECE == 0) {
 #pragma unroll
-                for (int i = 0; i < VPL; ++i) b[i] = (__bf16)o[i];
-                *reinterpret_cast<r_u32x4*>((__bf16*)a.d_logits + row + e) = __builtin_bit_cast(r_u32x4, b);
+            for (int i = 0; i < VPL; i += PIECE) {
+                if (e + i >= a.E) continue;
+                if constexpr (F32) {
+                    *reinterpret_cast<r_f32x4*>((float*)a.d_logits + row + e + i) = r_f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
+                } else {
+                    typedef __attribute__((ext_vector_type(8))) __bf16 r_bf16x8;
+                    r_bf16x8 b;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) b[c] = (__bf16)o[i + c];
+                    *reinterpret_cast<r_u32x4*>((__bf16*)a.d_logits + row + e + i) = __builtin_bit_cast(r_u32x4, b);
+                }
             }
         } else {
 #pragma unroll
@@ -309,6 +341,22 @@ template <bool F32> moe_status topk_of(const RouterArgs& a, bool wide, hipStream
     if (a.E <= 512) return launch_topk<F32, 64, 8>(a, wide, s);
     if (a.E <= 1024) return launch_topk<F32, 64, 16>(a, wide, s);
     return launch_topk<F32, 64, 64>(a, wide, s);
+}
+
+template <bool F32, int LANES, int VPL> moe_status launch_backward(const RouterArgs& a, bool wide, hipStream_t s) {
+    constexpr int PER = ROUTER_THREADS / LANES;
+    moe::LaunchScope k("router_backward_kernel", s);
+    const dim3 grid((unsigned)((a.T - 1) / PER + 1)), block(ROUTER_THREADS);
+    const int lds = PER * ((a.E + 3) & ~3) * (int)sizeof(float);           // (64 KiB for the most experts)
+    if (wide) hipLaunchKernelGGL((router_backward_kernel<F32, LANES, VPL, true>), grid, block, lds, s, a);
+    else hipLaunchKernelGGL((router_backward_kernel<F32, LANES, VPL, false>), grid, block, lds, s, a);
+    return k.done();
+}
+template <bool F32> moe_status backward_of(const RouterArgs& a, bool wide, hipStream_t s) {
+    if (a.topk <= 16 && a.E <= 64) return launch_backward<F32, 16, 4>(a, wide, s);
+    if (a.topk <= 16 && a.E <= 128) return launch_backward<F32, 16, 8>(a, wide, s);
+    if (a.E <= 256) return launch_backward<F32, 32, 8>(a, wide, s);
+    return launch_backward<F32, 64, 8>(a, wide, s);
 }
 
 moe_status checked(int T, int E, int topk, int logits_type, int score, int flags, float scale) {
@@ -341,14 +389,5 @@ extern "C" moe_status moe_router_topk_backward(const float* d_gates, const void*
     const RouterArgs a = {logits, ids, d_gates, nullptr, nullptr, d_logits, scale, T, E, topk, score, flags & MOE_ROUTER_RENORMALISE};
     const bool wide = (((uintptr_t)logits | (uintptr_t)d_logits) & 15) == 0 && E % (f32 ? 4 : 8) == 0;
     hipStream_t s = (hipStream_t)hip_stream;
-    const dim3 grid((unsigned)(((long long)T + 3) / 4)), block(ROUTER_THREADS);
-    moe::LaunchScope k("router_backward_kernel", s);
-    if (f32) {
-        if (wide) hipLaunchKernelGGL((router_backward_kernel<true, true>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((router_backward_kernel<true, false>), grid, block, 0, s, a);
-    } else {
-        if (wide) hipLaunchKernelGGL((router_backward_kernel<false, true>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((router_backward_kernel<false, false>), grid, block, 0, s, a);
-    }
-    return k.done();
+    return f32 ? backward_of<true>(a, wide, s) : backward_of<false>(a, wide, s);
 }
