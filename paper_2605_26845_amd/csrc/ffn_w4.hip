@@ -312,7 +312,7 @@ void ffn_w4_stream_kernel(W4Args a, int x_rows) {
 // in tiles of 64 x 256: 126 and 80 us, 750 and 590 TFLOP/s, matrix cores busy a third of the time; groups of 32 with zero points, in tiles of 64 x 128, 216 and 117.
 // Tiles of 128 x 256 (one wavefront per SIMD, whose sums spill to the matrix cores' half of the registers and are copied for every multiply-add): 196 and 110.
 template <int PHASE, int TM, int CW, int KS, int NC, int G, bool ZERO>
-__global__ __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1 : 2))) __launch_bounds__(CW * KS * 64)
+__global__ __attribute__((amdgpu_waves_per_eu(2))) __launch_bounds__(CW * KS * 64)
 void ffn_w4_tile_kernel(W4Args a) {
     static_assert(PHASE == 2 || NC % 2 == 0, "gate and up tiles in pairs");
     constexpr int THREADS = CW * KS * 64, TS = CW * 64, ROWS = 16 * TM, NI = ROWS * 16 / TS, NG = W4_STEP / G, PER = G / 32, D = NC == 4 ? 2 : 3, RB = NC == 4 ? 1 : 2;
@@ -548,12 +548,7 @@ void ffn_w4_tile_kernel(W4Args a) {
             }
     };
     // (row tiles beyond the last one are zeros, and not stored)
-    if constexpr (TM == 8) {
-        if (tiles <= 2) work(std::integral_constant<int, 2>{});
-        else if (tiles <= 4) work(std::integral_constant<int, 4>{});
-        else if (tiles <= 6) work(std::integral_constant<int, 6>{});
-        else work(std::integral_constant<int, 8>{});
-    } else if constexpr (TM == 4) {
+    if constexpr (TM == 4) {
         if (tiles <= 2) work(std::integral_constant<int, 2>{});
         else work(std::integral_constant<int, 4>{});
     } else {
@@ -564,7 +559,8 @@ void ffn_w4_tile_kernel(W4Args a) {
 
 template <int PHASE, int TM, int CW, int KS, int NC, int G, bool ZERO> moe_status launch_tile(const W4Args& a, hipStream_t s) {
     const int cols = (PHASE == 1 ? a.f : a.d) / (CW * 16 * (PHASE == 1 ? NC / 2 : NC));
-    moe::LaunchScope k(PHASE == 1 ? "ffn_w4_tile1_kernel" : "ffn_w4_tile2_kernel", s);
+    constexpr const char* NAMES[] = {"ffn_w4_small1_kernel", "ffn_w4_small2_kernel", "ffn_w4_middle1_kernel", "ffn_w4_middle2_kernel", "ffn_w4_large1_kernel", "ffn_w4_large2_kernel"};
+    moe::LaunchScope k(NAMES[(TM == 2 ? 0 : NC == 2 ? 2 : 4) + PHASE - 1], s);
     // (the kernel deals rows to dies in groups of eight)
     const dim3 grid = a.blocks ? dim3((unsigned)cols * (unsigned)((a.most_blocks + 7) / 8 * 8)) : dim3(cols, a.E, (a.M - 1) / (16 * TM) + 1);
     hipLaunchKernelGGL((ffn_w4_tile_kernel<PHASE, TM, CW, KS, NC, G, ZERO>), grid, dim3(CW * KS * 64), 0, s, a);

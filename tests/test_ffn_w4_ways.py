@@ -1,0 +1,83 @@
+"""moe_expert_ffn_w4_sliced: every kernel that its choice by sizes can take, named by the kernel timing, and rows far behind 2^31 bytes."""
+import numpy as np
+import pytest
+import torch
+
+from test_ffn_w4 import activations, check, offsets_of, run, weights
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+# group, M of M + 3 rows in the schedule, S, E, d, f, rows listed by expert first, kernels of the two products
+WAYS = [
+    (32, 1, 1, 1, 256, 1024, False, "small", "stream"),
+    (128, 1, 1, 8, 1024, 128, False, "stream", "small"),
+    (128, 5, 1000, 2, 1024, 1024, False, "small", "small"),
+    (32, 16, 1, 1, 4096, 128, False, "stream", "middle"),                  # 16 rows of 4096 do not fit LDS
+    (128, 16, 1, 1, 256, 4096, False, "small", "stream"),
+    (64, 33, 1, 2, 256, 4096, False, "middle", "small"),
+    (32, 17, 1, 1, 256, 128, False, "small", "middle"),
+    (128, 200, 1, 8, 256, 512, False, "middle", "small"),
+    (32, 200, 1, 8, 256, 512, False, "middle", "small"),
+    (128, 400, 1, 16, 256, 128, False, "middle", "middle"),
+    (128, 400, 1, 64, 256, 128, False, "middle", "large"),
+    (128, 1000, 1, 16, 256, 512, False, "large", "middle"),
+    (128, 2000, 3, 64, 256, 256, True, "middle", "middle"),
+    (32, 1, 2000, 1, 256, 128, True, "middle", "middle"),
+    (64, 700, 1200, 3, 256, 128, True, "middle", "middle"),
+    (128, 33, 1000, 64, 256, 512, True, "large", "middle"),
+    (128, 200, 1000, 64, 1024, 128, True, "middle", "large"),
+    (128, 3000, 1, 256, 256, 128, True, "large", "large"),
+]
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("group,M,S,E,d,f,listed,first,second", WAYS)
+def test_every_way(lib, group, M, S, E, d, f, listed, first, second, zeros):
+    rng = np.random.default_rng(M + S)
+    sizes = rng.multinomial(M, rng.dirichlet(np.full(S * E, 0.3)))        # uneven, most groups empty
+    off = offsets_of(sizes)
+    extra = 3
+    x, w = activations(M + extra, d, M), weights(E, d, f, group, zeros, M + d)
+    row_map = rng.permutation(M + extra).astype(np.int32)                 # its first M entries are the schedule's
+    row_gate = rng.random(M + extra).astype(np.float32)
+    y = torch.full((M + extra, d), 3.0, dtype=torch.bfloat16, device=DEV)
+    lib.moe_kernel_timing_enable(True)
+    try:
+        run(lib, x, off, S, E, w, y=y, row_map=torch.from_numpy(row_map).to(DEV), row_gate=torch.from_numpy(row_gate).to(DEV))
+        names = set(lib.moe_kernel_timing_read())
+    finally:
+        lib.moe_kernel_timing_enable(False)
+    print(names)
+    check_rows(y, x, off, E, w, row_map, row_gate)
+    assert "ffn_w4_%s1_kernel" % first in names and "ffn_w4_%s2_kernel" % second in names, names
+    assert ("ffn_plan_kernel" in names) == listed, names
+
+
+def check_rows(y, x, off, E, w, row_map, row_gate):
+    """test_ffn_w4.check for a map that names each row of x at most once and has as many entries as x has rows: the rows it leaves out keep their 3."""
+    M = int(off[-1])
+    order = torch.from_numpy(row_map[:M].astype(np.int64))
+    got = y.cpu()[order]
+    check(got, x[order], off, E, w, row_gate=row_gate[:M], kept=3.0)
+    left = np.setdiff1d(np.arange(len(x)), row_map[:M])
+    assert (y.cpu()[torch.from_numpy(left)].double() == 3.0).all()
+
+
+@pytest.mark.parametrize("M,d,f,zeros", [(131000, 16384, 128, True), (131000, 256, 16384, False)])
+def test_rows_behind_two_gib(lib, M, d, f, zeros):
+    """Rows at the end of 4 GiB of x, y and intermediates: the last ones against the oracle, all others with an expert whose scales are zero."""
+    E, S = 2, 1
+    last = 70
+    off = offsets_of([M - last, last])
+    w = weights(E, d, f, 128, zeros, 5)
+    for n in ("s_gate", "s_up", "s_down"):
+        w[n][0] = 0.0
+    tail = activations(last, d, 3)
+    x = torch.ones(M, d, dtype=torch.bfloat16, device=DEV)
+    x[M - last:] = tail.to(DEV)
+    c = {k: (None if v is None else v.to(DEV)) for k, v in w.items()}
+    y = lib.moe_expert_ffn_w4_sliced(x, torch.from_numpy(off).to(DEV), S, E, **c)
+    assert not y[: M - last].any().item()
+    one = {k: (None if v is None else v[1:]) for k, v in w.items()}
+    check(y[M - last:], tail, offsets_of([last]), 1, one)
