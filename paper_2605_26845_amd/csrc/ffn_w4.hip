@@ -317,7 +317,7 @@ void ffn_w4_tile_kernel(W4Args a) {
     static_assert(PHASE == 2 || NC % 2 == 0, "gate and up tiles in pairs");
     constexpr int THREADS = CW * KS * 64, TS = CW * 64, ROWS = 16 * TM, NI = ROWS * 16 / TS, NG = W4_STEP / G, PER = G / 32, D = NC == 4 ? 2 : 3, RB = NC == 4 ? 1 : 2;
     constexpr int NH = PHASE == 1 ? NC / 2 : NC;                           // column tiles of the output
-    constexpr int X_BYTES = ROWS * 256, S_BYTES = ROWS * NG * 4, SLICE = 3 * X_BYTES + 2 * S_BYTES;
+    constexpr int X_BYTES = ROWS * 256, SLICE = 2 * X_BYTES;
     constexpr int RED_BYTES = (KS - 1) * CW * NC * TM * 64 * 16, LDS = KS * SLICE > RED_BYTES ? KS * SLICE : RED_BYTES;
     __shared__ __attribute__((aligned(16))) unsigned char s_mem[LDS];
     __shared__ int s_row[ROWS], s_io[ROWS];                                // row of h; of x (phase 1) and y (phase 2)
@@ -385,13 +385,15 @@ void ffn_w4_tile_kernel(W4Args a) {
     const unsigned int qoff = (unsigned int)r16 * (unsigned int)(K / 2) + (unsigned int)g4 * 16u;
     const unsigned int soff = (unsigned int)(g4 % NG) * (unsigned int)NO + (unsigned int)r16;
     const int rot = (int)(((unsigned)col_tile * 3u + (unsigned)e * 3u) % (unsigned)KT);      // column tiles start at different steps of K
-    // step i of this slice, below KT: one behind its last is its last one again, and is not used; so is the first one of a slice that has none (ks >= KT)
-    const int ks0 = n > 0 ? ks : 0;
-    auto step_of = [&](int i) __attribute__((always_inline)) { const int kc = ks0 + KS * max(min(i, n - 1), 0) + rot; return kc >= KT ? kc - KT : kc; };
+    // The steps of this slice come round again behind its last one (what is loaded then is not used); a slice that has none (ks >= KT) starts at step 0.
+    const int kstep = KS % KT, kfirst = (n > 0 ? ks : 0) + rot;
+    auto next_step = [&](int& kc) __attribute__((always_inline)) { kc += kstep; if (kc >= KT) kc -= KT; };
+    int kx = kfirst >= KT ? kfirst - KT : kfirst, kq = kx;                 // of the next x and of the next codes to be loaded
 
     struct Codes { u32x4 q[NC]; unsigned int s[NC], z[NC]; };
-    auto load_codes = [&](Codes& b, int i) __attribute__((always_inline)) {
-        const unsigned int kc = (unsigned int)step_of(i);
+    auto load_codes = [&](Codes& b) __attribute__((always_inline)) {
+        const unsigned int kc = (unsigned int)kq;
+        next_step(kq);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const unsigned int so = soff + kc * NG * (unsigned int)NO;
@@ -405,9 +407,10 @@ void ffn_w4_tile_kernel(W4Args a) {
         constexpr int TI = (T * 256 + TS - 1) / TS;                        // pieces of x a thread copies per step
         unsigned char* const mem = s_mem + ks * SLICE;
         u32x4 xr[TI];
-        auto load_x = [&](int i) __attribute__((always_inline)) {
+        auto load_x = [&]() __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < TI; ++j) xr[j] = __builtin_amdgcn_raw_buffer_load_b128(rx, xoff[j], step_of(i) * (W4_STEP * 2), 0);
+            for (int j = 0; j < TI; ++j) xr[j] = __builtin_amdgcn_raw_buffer_load_b128(rx, xoff[j], kx * (W4_STEP * 2), 0);
+            next_step(kx);
         };
         auto put_x = [&](int buffer) __attribute__((always_inline)) {
 #pragma unroll
@@ -420,29 +423,13 @@ void ffn_w4_tile_kernel(W4Args a) {
             const int row = t * 16 + r16;
             return *reinterpret_cast<const bf16x8*>(mem + buffer * X_BYTES + row * 256 + ((k8_of<G>(i, g4) ^ row) & 15) * 16);
         };
-        auto sums_at = [&](int half) __attribute__((always_inline)) { return (float*)(mem + 3 * X_BYTES + half * S_BYTES); };
-        // what the sums over a step's groups start at, for every CW-th row tile
-        auto put_sums = [&](int buffer, int half) __attribute__((always_inline)) {
-            const bf16x8 constant = splat(ZERO ? MINUS_48 : MINUS_24);
-#pragma unroll
-            for (int t0 = 0; t0 < T; t0 += CW) {
-                const int t = t0 + cw;
-                if (T % CW != 0 && t >= T) break;
-                f32x4 s[NG];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[i / PER] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fragment(buffer, t, i), constant, i % PER == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[i / PER], 0, 0, 0);
-                if (r16 == 0) {
-#pragma unroll
-                    for (int gr = 0; gr < NG; ++gr) *reinterpret_cast<f32x4*>(sums_at(half) + gr * ROWS + t * 16 + 4 * g4) = s[gr];
-                }
-            }
-        };
+        const bf16x8 constant = splat(ZERO ? MINUS_48 : MINUS_24);
         f32x4 acc[NC][T];
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int t = 0; t < T; ++t) acc[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-        auto multiply = [&](Codes& b, int buffer, int half) __attribute__((always_inline)) {
+        auto multiply = [&](Codes& b, int buffer) __attribute__((always_inline)) {
             bf16x8 w[NC][4];
             float scale[NC][NG];
 #pragma unroll
@@ -459,12 +446,10 @@ void ffn_w4_tile_kernel(W4Args a) {
                 }
             }
             // row tile by row tile, the fragments of the next one on their way from LDS (not more: registers)
-            struct Rows { bf16x8 x[4]; f32x4 sums[NG]; } rb[RB];
+            struct Rows { bf16x8 x[4]; } rb[RB];
             auto fetch = [&](Rows& r, int t) __attribute__((always_inline)) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) r.x[i] = fragment(buffer, t, i);
-#pragma unroll
-                for (int gr = 0; gr < NG; ++gr) r.sums[gr] = *reinterpret_cast<const f32x4*>(sums_at(half) + gr * ROWS + t * 16 + 4 * g4);
             };
             if (RB == 2) fetch(rb[0], 0);
 #pragma unroll
@@ -474,11 +459,13 @@ void ffn_w4_tile_kernel(W4Args a) {
                 const Rows& r = rb[t % RB];
 #pragma unroll
                 for (int gr = 0; gr < NG; ++gr) {
-                    f32x4 sum[NC];
+                    f32x4 sum[NC], start = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = gr * PER; i < (gr + 1) * PER; ++i) start = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r.x[i], constant, start, 0, 0, 0);
 #pragma unroll
                     for (int i = gr * PER; i < (gr + 1) * PER; ++i)
 #pragma unroll
-                        for (int c = 0; c < NC; ++c) sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r.x[i], w[c][i], i == gr * PER ? r.sums[gr] : sum[c], 0, 0, 0);
+                        for (int c = 0; c < NC; ++c) sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r.x[i], w[c][i], i == gr * PER ? start : sum[c], 0, 0, 0);
 #pragma unroll
                     for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -488,30 +475,24 @@ void ffn_w4_tile_kernel(W4Args a) {
             }
         };
         Codes codes[D];
-        load_x(0);
+        load_x();
 #pragma unroll
-        for (int i = 0; i < D - 1; ++i) load_codes(codes[i], i);
+        for (int i = 0; i < D - 1; ++i) load_codes(codes[i]);
         put_x(0);
-        load_x(1);
         moe::lds_only_barrier();
-        put_sums(0, 0);
-        put_x(1);
-        moe::lds_only_barrier();
-        // step i: x and its sums are in LDS, x of step i + 1 too; the buffer of step i + 2 was last read in step i - 1
+        // step i: its x is in LDS; the buffer of step i + 1 was last read in step i - 1
         int buffer = 0;
         for (int i = 0; i < n_most; i += D) {
 #pragma unroll
             for (int u = 0; u < D; ++u) {
                 if (i + u >= n_most) break;
-                const int second = buffer + 1 >= 3 ? buffer - 2 : buffer + 1, third = buffer + 2 >= 3 ? buffer - 1 : buffer + 2;
-                load_x(i + u + 2);
-                load_codes(codes[(u + D - 1) % D], i + u + D - 1);
+                load_x();
+                load_codes(codes[(u + D - 1) % D]);
                 __builtin_amdgcn_sched_barrier(0);
-                put_sums(second, (i + u + 1) & 1);
-                if (i + u < n) multiply(codes[u], buffer, (i + u) & 1);
-                put_x(third);
+                if (i + u < n) multiply(codes[u], buffer);
+                buffer ^= 1;
+                put_x(buffer);
                 moe::lds_only_barrier();
-                buffer = second;
             }
         }
         if constexpr (KS > 1) {
@@ -559,8 +540,8 @@ void ffn_w4_tile_kernel(W4Args a) {
 
 template <int PHASE, int TM, int CW, int KS, int NC, int G, bool ZERO> moe_status launch_tile(const W4Args& a, hipStream_t s) {
     const int cols = (PHASE == 1 ? a.f : a.d) / (CW * 16 * (PHASE == 1 ? NC / 2 : NC));
-    constexpr const char* NAMES[] = {"ffn_w4_small1_kernel", "ffn_w4_small2_kernel", "ffn_w4_middle1_kernel", "ffn_w4_middle2_kernel", "ffn_w4_large1_kernel", "ffn_w4_large2_kernel"};
-    moe::LaunchScope k(NAMES[(TM == 2 ? 0 : NC == 2 ? 2 : 4) + PHASE - 1], s);
+    constexpr const char* NAMES[] = {"ffn_w4_small1_kernel", "ffn_w4_small2_kernel", "ffn_w4_middle1_kernel", "ffn_w4_middle2_kernel", "ffn_w4_large1_kernel", "ffn_w4_large2_kernel", "ffn_w4_tall1_kernel", "ffn_w4_tall2_kernel"};
+    moe::LaunchScope k(NAMES[(TM == 2 ? 0 : CW == 2 ? 6 : NC == 2 ? 2 : 4) + PHASE - 1], s);
     // (the kernel deals rows to dies in groups of eight)
     const dim3 grid = a.blocks ? dim3((unsigned)cols * (unsigned)((a.most_blocks + 7) / 8 * 8)) : dim3(cols, a.E, (a.M - 1) / (16 * TM) + 1);
     hipLaunchKernelGGL((ffn_w4_tile_kernel<PHASE, TM, CW, KS, NC, G, ZERO>), grid, dim3(CW * KS * 64), 0, s, a);
@@ -598,7 +579,7 @@ template <int PHASE, bool XLDS, int G, bool ZERO> moe_status launch_stream(const
 //   E 4, d 7168, f 2048:    1 row 14+14  19+9   39+14  63+21,   24 rows 36+17  24+13  41+16  64+22,   200 rows -  44+28  57+26  97+33,  1000 rows -  159+108  115+51  124+45
 //   E 4, d 2048, f 1408:    1 row 12+7   10+7   14+11  20+16,   200 rows -  20+12  21+16  32+25,  2500 rows -  -  61+33  60+33,  8191 rows -  -  151+83  126+80
 // (64 x 256 tiles in smaller groups: 2500 rows of the last, groups of 64, 67+36 and 81+40: the scales of more groups do not fit its registers.)
-enum Way { W4_STREAM, W4_SMALL, W4_MIDDLE, W4_LARGE };
+enum Way { W4_STREAM, W4_SMALL, W4_MIDDLE, W4_LARGE, W4_TALL };
 struct TileTimes { int rows, weight_rows, slices; double few, full, shared; };      // a step alone on its compute unit with up to half the rows, with all; its share of a full one
 constexpr TileTimes SMALL_TILE = {32, 64, 2, 0.55, 0.75, 0.60}, MIDDLE_TILE = {64, 128, 1, 0.65, 0.88, 0.70}, LARGE_TILE = {64, 256, 1, 1.05, 1.6, 1.25};
 
@@ -641,6 +622,7 @@ template <int PHASE, int G, bool ZERO> moe_status launch_way(Way way, const W4Ar
             return rows * (K * 2 + 16) <= STREAM_X_MOST ? launch_stream<PHASE, true, G, ZERO>(a, rows, s) : launch_stream<PHASE, false, G, ZERO>(a, rows, s);
         }
         case W4_SMALL: return launch_tile<PHASE, 2, 2, 2, 2, G, ZERO>(a, s);
+        case W4_TALL: return launch_tile<PHASE, 4, 2, 2, 2, G, ZERO>(a, s);
         case W4_LARGE:
             if constexpr (G == 128) return launch_tile<PHASE, 4, 4, 1, 4, G, ZERO>(a, s);
         default: return launch_tile<PHASE, 4, 4, 1, 2, G, ZERO>(a, s);
