@@ -430,48 +430,49 @@ void ffn_w4_tile_kernel(W4Args a) {
 #pragma unroll
             for (int t = 0; t < T; ++t) acc[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
         auto multiply = [&](Codes& b, int buffer) __attribute__((always_inline)) {
-            bf16x8 w[NC][4];
-            float scale[NC][NG];
+            unsigned int sz[NC][NG];
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 across_lanes<G>(b.q[c]);
-                unsigned int sz[NG];
-                all_groups<NG>(scale_and_zero<ZERO>(b.s[c], b.z[c], r16), sz);
-#pragma unroll
-                for (int gr = 0; gr < NG; ++gr) {
-                    scale[c][gr] = __builtin_bit_cast(float, sz[gr] & 0xFFFF0000u) * CODE_UNIT;
-                    const unsigned int base = code_base<ZERO>(sz[gr]);
-#pragma unroll
-                    for (int i = gr * PER; i < (gr + 1) * PER; ++i) w[c][i] = code_values<ZERO>(b.q[c][i], base, mask);
-                }
+                all_groups<NG>(scale_and_zero<ZERO>(b.s[c], b.z[c], r16), sz[c]);
             }
-            // row tile by row tile, the fragments of the next one on their way from LDS (not more: registers)
-            struct Rows { bf16x8 x[4]; } rb[RB];
-            auto fetch = [&](Rows& r, int t) __attribute__((always_inline)) {
+            // group by group, row tile by row tile, the fragments of the next row tile on their way from LDS (not more: registers)
+            struct Rows { bf16x8 x[PER]; } rb[RB];
+            auto fetch = [&](Rows& r, int gr, int t) __attribute__((always_inline)) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) r.x[i] = fragment(buffer, t, i);
+                for (int i = 0; i < PER; ++i) r.x[i] = fragment(buffer, t, gr * PER + i);
             };
-            if (RB == 2) fetch(rb[0], 0);
+            if (RB == 2) fetch(rb[0], 0, 0);
 #pragma unroll
-            for (int t = 0; t < T; ++t) {
-                if (RB == 1) fetch(rb[0], t);
-                else if (t + 1 < T) fetch(rb[(t + 1) % RB], t + 1);
-                const Rows& r = rb[t % RB];
+            for (int gr = 0; gr < NG; ++gr) {
+                bf16x8 w[NC][PER];
+                float scale[NC];
 #pragma unroll
-                for (int gr = 0; gr < NG; ++gr) {
+                for (int c = 0; c < NC; ++c) {
+                    scale[c] = __builtin_bit_cast(float, sz[c][gr] & 0xFFFF0000u) * CODE_UNIT;
+                    const unsigned int base = code_base<ZERO>(sz[c][gr]);
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) w[c][i] = code_values<ZERO>(b.q[c][gr * PER + i], base, mask);
+                }
+#pragma unroll
+                for (int t = 0; t < T; ++t) {
+                    const int at = gr * T + t;
+                    if (RB == 1) fetch(rb[0], gr, t);
+                    else if (at + 1 < NG * T) fetch(rb[(at + 1) % RB], (at + 1) / T, (at + 1) % T);
+                    const Rows& r = rb[at % RB];
                     f32x4 sum[NC], start = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int i = gr * PER; i < (gr + 1) * PER; ++i) start = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r.x[i], constant, start, 0, 0, 0);
+                    for (int i = 0; i < PER; ++i) start = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r.x[i], constant, start, 0, 0, 0);
 #pragma unroll
-                    for (int i = gr * PER; i < (gr + 1) * PER; ++i)
+                    for (int i = 0; i < PER; ++i)
 #pragma unroll
-                        for (int c = 0; c < NC; ++c) sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r.x[i], w[c][i], i == gr * PER ? start : sum[c], 0, 0, 0);
+                        for (int c = 0; c < NC; ++c) sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r.x[i], w[c][i], i == 0 ? start : sum[c], 0, 0, 0);
 #pragma unroll
                     for (int c = 0; c < NC; ++c)
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) acc[c][t][v] = __builtin_fmaf(scale[c][gr], sum[c][v], acc[c][t][v]);
+                        for (int v = 0; v < 4; ++v) acc[c][t][v] = __builtin_fmaf(scale[c], sum[c][v], acc[c][t][v]);
+                    if (PER * NC > 4) __builtin_amdgcn_sched_barrier(0);
                 }
-                __builtin_amdgcn_sched_barrier(0);
             }
         };
         Codes codes[D];
