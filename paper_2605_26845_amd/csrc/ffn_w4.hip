@@ -252,7 +252,7 @@ void ffn_w4_stream_kernel(W4Args a, int x_rows) {
 #pragma unroll
                 for (int i = gr * PER; i < (gr + 1) * PER; ++i)
                     sum[gr] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r[i]), code_values<ZERO>(b.q[i], base, mask), sum[gr], 0, 0, 0);
-                const float scale = __builtin_bit_cast(float, sz[gr] & 0xFFFF0000u) * CODE_UNIT;
+                const float scale = __builtin_bit_cast(float, sz[gr] & 0xFFFF0000u);
 #pragma unroll
                 for (int v = 0; v < 4; ++v) acc[v] = __builtin_fmaf(scale, sum[gr][v], acc[v]);
             }
@@ -276,8 +276,8 @@ void ffn_w4_stream_kernel(W4Args a, int x_rows) {
                     }
                     const int m = s_row[m16], o = strip * COLS + col;
                     // the hidden activation is rounded to bf16 once, as the operand of the second product
-                    if (PHASE == 1) a.h[(size_t)m * a.f + o] = (__bf16)(silu(s0) * s1);
-                    else a.y[(size_t)w4_mapped(a, m) * a.d + o] = (__bf16)(a.row_gate ? a.row_gate[m] * s0 : s0);
+                    if (PHASE == 1) a.h[(size_t)m * a.f + o] = (__bf16)(silu(CODE_UNIT * s0) * (CODE_UNIT * s1));
+                    else a.y[(size_t)w4_mapped(a, m) * a.d + o] = (__bf16)((a.row_gate ? a.row_gate[m] : 1.0f) * (CODE_UNIT * s0));
                 }
             }
             half ^= 1;
@@ -312,10 +312,10 @@ void ffn_w4_stream_kernel(W4Args a, int x_rows) {
 // in tiles of 64 x 256: 126 and 80 us, 750 and 590 TFLOP/s, matrix cores busy a third of the time; groups of 32 with zero points, in tiles of 64 x 128, 216 and 117.
 // Tiles of 128 x 256 (one wavefront per SIMD, whose sums spill to the matrix cores' half of the registers and are copied for every multiply-add): 196 and 110.
 template <int PHASE, int TM, int CW, int KS, int NC, int G, bool ZERO>
-__global__ __attribute__((amdgpu_waves_per_eu(2))) __launch_bounds__(CW * KS * 64)
+__global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(CW * KS * 64)
 void ffn_w4_tile_kernel(W4Args a) {
     static_assert(PHASE == 2 || NC % 2 == 0, "gate and up tiles in pairs");
-    constexpr int THREADS = CW * KS * 64, TS = CW * 64, ROWS = 16 * TM, NI = ROWS * 16 / TS, NG = W4_STEP / G, PER = G / 32, D = NC == 4 ? 2 : 3, RB = NC == 4 ? 1 : 2;
+    constexpr int THREADS = CW * KS * 64, TS = CW * 64, ROWS = 16 * TM, NI = ROWS * 16 / TS, NG = W4_STEP / G, PER = G / 32, D = 2, RB = NC == 4 ? 1 : 2;
     constexpr int NH = PHASE == 1 ? NC / 2 : NC;                           // column tiles of the output
     constexpr int X_BYTES = ROWS * 256, SLICE = 2 * X_BYTES;
     constexpr int RED_BYTES = (KS - 1) * CW * NC * TM * 64 * 16, LDS = KS * SLICE > RED_BYTES ? KS * SLICE : RED_BYTES;
@@ -329,222 +329,230 @@ void ffn_w4_tile_kernel(W4Args a) {
     unsigned int mask = MASK<ZERO>;
     asm("" : "+v"(mask));
     int e, rows, col_tile;
-    if (a.blocks) {
-        // neighbouring workgroups of a die (every eighth one) take the column tiles of one row block, whose rows then stay in its L2; with few row blocks
-        // the dies share them
-        const int cols = NO / (CW * NH * 16), blocks = a.blocks[0].x, id = blockIdx.x;
-        int block;
-        if (blocks >= 32) { const int i = id >> 3; block = i / cols * 8 + (id & 7); col_tile = i % cols; }
-        else { block = id / cols; col_tile = id % cols; }
-        if (block >= blocks) return;
-        const int4 b = a.blocks[a.first_block + block];
-        e = __builtin_amdgcn_readfirstlane(b.z);
-        rows = __builtin_amdgcn_readfirstlane(min(b.y - b.x, ROWS));
-        for (int i = tid; i < rows; i += THREADS) {
-            s_row[i] = b.x + i;
-            s_io[i] = a.list[b.x + i];
-            if (PHASE == 2) s_gate[i] = a.list_gate ? a.list_gate[b.x + i] : 1.0f;
+    for (int z = blockIdx.z;; z += gridDim.z) {                            // (a workgroup that follows a list has one block; so have the largest tiles, whose registers a loop would spill)
+        if (a.blocks) {
+            // neighbouring workgroups of a die (every eighth one) take the column tiles of one row block, whose rows then stay in its L2; with few row blocks
+            // the dies share them
+            const int cols = NO / (CW * NH * 16), blocks = a.blocks[0].x, id = blockIdx.x;
+            int block;
+            if (blocks >= 32) { const int i = id >> 3; block = i / cols * 8 + (id & 7); col_tile = i % cols; }
+            else { block = id / cols; col_tile = id % cols; }
+            if (block >= blocks) return;
+            const int4 b = a.blocks[a.first_block + block];
+            e = __builtin_amdgcn_readfirstlane(b.z);
+            rows = __builtin_amdgcn_readfirstlane(min(b.y - b.x, ROWS));
+            for (int i = tid; i < rows; i += THREADS) {
+                s_row[i] = b.x + i;
+                s_io[i] = a.list[b.x + i];
+                if (PHASE == 2) s_gate[i] = a.list_gate ? a.list_gate[b.x + i] : 1.0f;
+            }
+        } else {
+            col_tile = blockIdx.x;
+            e = blockIdx.y;
+            const int first = z * ROWS;
+            rows = min(expert_rows<THREADS, ROWS>(a, e, first, s_row, s_scan) - first, ROWS);
+            if (rows <= 0) return;
+            for (int i = tid; i < rows; i += THREADS) {
+                const int m = s_row[i];
+                s_io[i] = w4_mapped(a, m);
+                if (PHASE == 2) s_gate[i] = a.row_gate ? a.row_gate[m] : 1.0f;
+            }
         }
-    } else {
-        col_tile = blockIdx.x;
-        e = blockIdx.y;
-        const int first = (int)blockIdx.z * ROWS;
-        rows = min(expert_rows<THREADS, ROWS>(a, e, first, s_row, s_scan) - first, ROWS);
-        if (rows <= 0) return;
-        for (int i = tid; i < rows; i += THREADS) {
-            const int m = s_row[i];
-            s_io[i] = w4_mapped(a, m);
-            if (PHASE == 2) s_gate[i] = a.row_gate ? a.row_gate[m] : 1.0f;
+        __syncthreads();
+        const int tiles = (rows + 15) / 16;
+        const int col0 = (col_tile * CW + cw) * NH * 16;
+        const int KT = K / W4_STEP, n = (KT - ks + KS - 1) / KS, n_most = (KT + KS - 1) / KS;      // steps of this slice, of any slice
+
+        // ---- what a thread copies: chunk `chunk` of rows row0, row0 + TS / 16, ...
+        const int ts = tid % TS, chunk = ts & 15, row0 = ts >> 4;
+        const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)(PHASE == 1 ? (const void*)a.x : (const void*)a.h), 0, (unsigned int)a.M * (unsigned int)K * 2u, 0x00020000);
+        unsigned int xoff[NI];
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int r = row0 + i * (TS / 16);
+            xoff[i] = r < rows ? (unsigned int)(PHASE == 1 ? s_io[r] : s_row[r]) * (unsigned int)K * 2u + (unsigned int)chunk * 16u : 0xFFFFFF00u;      // past the end: zeros
         }
-    }
-    __syncthreads();
-    const int tiles = (rows + 15) / 16;
-    const int col0 = (col_tile * CW + cw) * NH * 16;
-    const int KT = K / W4_STEP, n = (KT - ks + KS - 1) / KS, n_most = (KT + KS - 1) / KS;      // steps of this slice, of any slice
-
-    // ---- what a thread copies: chunk `chunk` of rows row0, row0 + TS / 16, ...
-    const int ts = tid % TS, chunk = ts & 15, row0 = ts >> 4;
-    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)(PHASE == 1 ? (const void*)a.x : (const void*)a.h), 0, (unsigned int)a.M * (unsigned int)K * 2u, 0x00020000);
-    unsigned int xoff[NI];
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-        const int r = row0 + i * (TS / 16);
-        xoff[i] = r < rows ? (unsigned int)(PHASE == 1 ? s_io[r] : s_row[r]) * (unsigned int)K * 2u + (unsigned int)chunk * 16u : 0xFFFFFF00u;      // past the end: zeros
-    }
-    const unsigned char* qbase[NC];
-    const unsigned short* sbase[NC];
-    const unsigned char* zbase[NC];
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        const int col = col0 + (c % NH) * 16;
-        const size_t row = (size_t)e * NO + col, group = (size_t)e * (K / G) * NO + col;
-        qbase[c] = (PHASE == 2 ? a.qd : c >= NH ? a.qu : a.qg) + row * (size_t)(K / 2);
-        sbase[c] = (PHASE == 2 ? a.sd : c >= NH ? a.su : a.sg) + group;
-        zbase[c] = ZERO ? (PHASE == 2 ? a.zd : c >= NH ? a.zu : a.zg) + group : nullptr;
-    }
-    const unsigned int qoff = (unsigned int)r16 * (unsigned int)(K / 2) + (unsigned int)g4 * 16u;
-    const unsigned int soff = (unsigned int)(g4 % NG) * (unsigned int)NO + (unsigned int)r16;
-    const int rot = (int)(((unsigned)col_tile * 3u + (unsigned)e * 3u) % (unsigned)KT);      // column tiles start at different steps of K
-    // The steps of this slice come round again behind its last one (what is loaded then is not used); a slice that has none (ks >= KT) starts at step 0.
-    const int kstep = KS % KT, kfirst = (n > 0 ? ks : 0) + rot;
-    auto next_step = [&](int& kc) __attribute__((always_inline)) { kc += kstep; if (kc >= KT) kc -= KT; };
-    int kx = kfirst >= KT ? kfirst - KT : kfirst, kq = kx;                 // of the next x and of the next codes to be loaded
-
-    struct Codes { u32x4 q[NC]; unsigned int s[NC], z[NC]; };
-    auto load_codes = [&](Codes& b) __attribute__((always_inline)) {
-        const unsigned int kc = (unsigned int)kq;
-        next_step(kq);
+        const unsigned char* qbase[NC];
+        const unsigned short* sbase[NC];
+        const unsigned char* zbase[NC];
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            const unsigned int so = soff + kc * NG * (unsigned int)NO;
-            b.q[c] = *reinterpret_cast<const u32x4*>(qbase[c] + (qoff + kc * (W4_STEP / 2)));
-            b.s[c] = *reinterpret_cast<const unsigned int*>(sbase[c] + (so & ~1u));
-            if (ZERO) b.z[c] = *reinterpret_cast<const unsigned int*>(zbase[c] + (so & ~3u));
+            const int col = col0 + (c % NH) * 16;
+            const size_t row = (size_t)e * NO + col, group = (size_t)e * (K / G) * NO + col;
+            qbase[c] = (PHASE == 2 ? a.qd : c >= NH ? a.qu : a.qg) + row * (size_t)(K / 2);
+            sbase[c] = (PHASE == 2 ? a.sd : c >= NH ? a.su : a.sg) + group;
+            zbase[c] = ZERO ? (PHASE == 2 ? a.zd : c >= NH ? a.zu : a.zg) + group : nullptr;
         }
-    };
-    auto work = [&](auto tag) __attribute__((always_inline)) {
-        constexpr int T = decltype(tag)::value;                            // row tiles
-        constexpr int TI = (T * 256 + TS - 1) / TS;                        // pieces of x a thread copies per step
-        unsigned char* const mem = s_mem + ks * SLICE;
-        u32x4 xr[TI];
-        auto load_x = [&]() __attribute__((always_inline)) {
-#pragma unroll
-            for (int j = 0; j < TI; ++j) xr[j] = __builtin_amdgcn_raw_buffer_load_b128(rx, xoff[j], kx * (W4_STEP * 2), 0);
-            next_step(kx);
-        };
-        auto put_x = [&](int buffer) __attribute__((always_inline)) {
-#pragma unroll
-            for (int j = 0; j < TI; ++j) {
-                const int row = row0 + j * (TS / 16);
-                *reinterpret_cast<u32x4*>(mem + buffer * X_BYTES + row * 256 + ((chunk ^ row) & 15) * 16) = xr[j];
-            }
-        };
-        auto fragment = [&](int buffer, int t, int i) __attribute__((always_inline)) {
-            const int row = t * 16 + r16;
-            return *reinterpret_cast<const bf16x8*>(mem + buffer * X_BYTES + row * 256 + ((k8_of<G>(i, g4) ^ row) & 15) * 16);
-        };
-        const bf16x8 constant = splat(ZERO ? MINUS_48 : MINUS_24);
-        f32x4 acc[NC][T];
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int t = 0; t < T; ++t) acc[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-        auto multiply = [&](Codes& b, int buffer) __attribute__((always_inline)) {
-            unsigned int sz[NC][NG];
+        const unsigned int qoff = (unsigned int)r16 * (unsigned int)(K / 2) + (unsigned int)g4 * 16u;
+        const unsigned int soff = (unsigned int)(g4 % NG) * (unsigned int)NO + (unsigned int)r16;
+        // The steps of this slice come round again behind its last one (what is loaded then is not used); a slice that has none (ks >= KT) starts at step 0.
+        const int kstep = KS % KT;
+        auto next_step = [&](int& kc) __attribute__((always_inline)) { kc += kstep; if (kc >= KT) kc -= KT; };
+        int kx = n > 0 ? ks : 0, kq = kx;                                      // of the next x and of the next codes to be loaded
+
+        struct Codes { u32x4 q[NC]; unsigned int s[NC], z[NC]; };
+        auto load_codes = [&](Codes& b) __attribute__((always_inline)) {
+            const unsigned int kc = (unsigned int)kq;
+            next_step(kq);
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-                across_lanes<G>(b.q[c]);
-                all_groups<NG>(scale_and_zero<ZERO>(b.s[c], b.z[c], r16), sz[c]);
+                const unsigned int so = soff + kc * NG * (unsigned int)NO;
+                b.q[c] = *reinterpret_cast<const u32x4*>(qbase[c] + (qoff + kc * (W4_STEP / 2)));
+                b.s[c] = *reinterpret_cast<const unsigned int*>(sbase[c] + (so & ~1u));
+                if (ZERO) b.z[c] = *reinterpret_cast<const unsigned int*>(zbase[c] + (so & ~3u));
             }
-            // group by group, row tile by row tile, the fragments of the next row tile on their way from LDS (not more: registers)
-            struct Rows { bf16x8 x[PER]; } rb[RB];
-            auto fetch = [&](Rows& r, int gr, int t) __attribute__((always_inline)) {
+        };
+        auto work = [&](auto tag) __attribute__((always_inline)) {
+            constexpr int T = decltype(tag)::value;                            // row tiles
+            constexpr int TI = (T * 256 + TS - 1) / TS;                        // pieces of x a thread copies per step
+            unsigned char* const mem = s_mem + ks * SLICE;
+            u32x4 xr[TI];
+            auto load_x = [&]() __attribute__((always_inline)) {
 #pragma unroll
-                for (int i = 0; i < PER; ++i) r.x[i] = fragment(buffer, t, gr * PER + i);
+                for (int j = 0; j < TI; ++j) xr[j] = __builtin_amdgcn_raw_buffer_load_b128(rx, xoff[j], kx * (W4_STEP * 2), 0);
+                next_step(kx);
             };
-            if (RB == 2) fetch(rb[0], 0, 0);
+            auto put_x = [&](int buffer) __attribute__((always_inline)) {
 #pragma unroll
-            for (int gr = 0; gr < NG; ++gr) {
-                bf16x8 w[NC][PER];
-                float scale[NC];
+                for (int j = 0; j < TI; ++j) {
+                    const int row = row0 + j * (TS / 16);
+                    *reinterpret_cast<u32x4*>(mem + buffer * X_BYTES + row * 256 + ((chunk ^ row) & 15) * 16) = xr[j];
+                }
+            };
+            auto fragment = [&](int buffer, int t, int i) __attribute__((always_inline)) {
+                const int row = t * 16 + r16;
+                return *reinterpret_cast<const bf16x8*>(mem + buffer * X_BYTES + row * 256 + ((k8_of<G>(i, g4) ^ row) & 15) * 16);
+            };
+            const bf16x8 constant = splat(ZERO ? MINUS_48 : MINUS_24);
+            f32x4 acc[NC][T];
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int t = 0; t < T; ++t) acc[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            auto multiply = [&](Codes& b, int buffer) __attribute__((always_inline)) {
+                unsigned int sz[NC][NG];
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
-                    scale[c] = __builtin_bit_cast(float, sz[c][gr] & 0xFFFF0000u) * CODE_UNIT;
-                    const unsigned int base = code_base<ZERO>(sz[c][gr]);
-#pragma unroll
-                    for (int i = 0; i < PER; ++i) w[c][i] = code_values<ZERO>(b.q[c][gr * PER + i], base, mask);
+                    across_lanes<G>(b.q[c]);
+                    all_groups<NG>(scale_and_zero<ZERO>(b.s[c], b.z[c], r16), sz[c]);
                 }
+                // group by group, row tile by row tile, the fragments of the next row tile on their way from LDS (not more: registers)
+                struct Rows { bf16x8 x[PER]; } rb[RB];
+                auto fetch = [&](Rows& r, int gr, int t) __attribute__((always_inline)) {
 #pragma unroll
-                for (int t = 0; t < T; ++t) {
-                    const int at = gr * T + t;
-                    if (RB == 1) fetch(rb[0], gr, t);
-                    else if (at + 1 < NG * T) fetch(rb[(at + 1) % RB], (at + 1) / T, (at + 1) % T);
-                    const Rows& r = rb[at % RB];
-                    f32x4 sum[NC], start = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int i = 0; i < PER; ++i) r.x[i] = fragment(buffer, t, gr * PER + i);
+                };
+                if (RB == 2) fetch(rb[0], 0, 0);
 #pragma unroll
-                    for (int i = 0; i < PER; ++i) start = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r.x[i], constant, start, 0, 0, 0);
+                for (int gr = 0; gr < NG; ++gr) {
+                    bf16x8 w[NC][PER];
+                    float scale[NC];
 #pragma unroll
-                    for (int i = 0; i < PER; ++i)
+                    for (int c = 0; c < NC; ++c) {
+                        scale[c] = __builtin_bit_cast(float, sz[c][gr] & 0xFFFF0000u);
+                        const unsigned int base = code_base<ZERO>(sz[c][gr]);
 #pragma unroll
-                        for (int c = 0; c < NC; ++c) sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r.x[i], w[c][i], i == 0 ? start : sum[c], 0, 0, 0);
+                        for (int i = 0; i < PER; ++i) w[c][i] = code_values<ZERO>(b.q[c][gr * PER + i], base, mask);
+                    }
+#pragma unroll
+                    for (int t = 0; t < T; ++t) {
+                        const int at = gr * T + t;
+                        if (RB == 1) fetch(rb[0], gr, t);
+                        else if (at + 1 < NG * T) fetch(rb[(at + 1) % RB], (at + 1) / T, (at + 1) % T);
+                        const Rows& r = rb[at % RB];
+                        f32x4 sum[NC], start = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int i = 0; i < PER; ++i) start = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r.x[i], constant, start, 0, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < PER; ++i)
+#pragma unroll
+                            for (int c = 0; c < NC; ++c) sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r.x[i], w[c][i], i == 0 ? start : sum[c], 0, 0, 0);
+#pragma unroll
+                        for (int c = 0; c < NC; ++c)
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) acc[c][t][v] = __builtin_fmaf(scale[c], sum[c][v], acc[c][t][v]);
+                        if (PER * NC > 4) __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+            };
+            Codes codes[D];
+            load_x();
+#pragma unroll
+            for (int i = 0; i < D - 1; ++i) load_codes(codes[i]);
+            put_x(0);
+            moe::lds_only_barrier();
+            // step i: its x is in LDS; the buffer of step i + 1 was last read in step i - 1
+            int buffer = 0;
+            for (int i = 0; i < n_most; i += D) {
+#pragma unroll
+                for (int u = 0; u < D; ++u) {
+                    if (i + u >= n_most) break;
+                    load_x();
+                    load_codes(codes[(u + D - 1) % D]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (i + u < n) multiply(codes[u], buffer);
+                    buffer ^= 1;
+                    put_x(buffer);
+                    moe::lds_only_barrier();
+                }
+            }
+            if constexpr (KS > 1) {
+                f32x4* const red = (f32x4*)s_mem;
+                if (ks > 0) {
 #pragma unroll
                     for (int c = 0; c < NC; ++c)
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) acc[c][t][v] = __builtin_fmaf(scale[c], sum[c][v], acc[c][t][v]);
-                    if (PER * NC > 4) __builtin_amdgcn_sched_barrier(0);
+                        for (int t = 0; t < T; ++t) red[((((ks - 1) * CW + cw) * NC + c) * T + t) * 64 + lane] = acc[c][t];
                 }
+                __syncthreads();
+                if (ks > 0) return;
+#pragma unroll
+                for (int s = 1; s < KS; ++s)
+#pragma unroll
+                    for (int c = 0; c < NC; ++c)
+#pragma unroll
+                        for (int t = 0; t < T; ++t) acc[c][t] += red[((((s - 1) * CW + cw) * NC + c) * T + t) * 64 + lane];
             }
+            // ---- acc[c][t][v]: row 4 * g4 + v of row tile t, column r16 of column tile c
+#pragma unroll
+            for (int t = 0; t < T; ++t)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const int r = t * 16 + 4 * g4 + v;
+                    if (r >= rows) continue;
+#pragma unroll
+                    for (int c = 0; c < NH; ++c) {
+                        const int o = col0 + c * 16 + r16;
+                        // the hidden activation is rounded to bf16 once, as the operand of the second product
+                        if constexpr (PHASE == 1) a.h[(size_t)s_row[r] * a.f + o] = (__bf16)(silu(CODE_UNIT * acc[c][t][v]) * (CODE_UNIT * acc[NH + c][t][v]));
+                        else a.y[(size_t)s_io[r] * a.d + o] = (__bf16)(s_gate[r] * (CODE_UNIT * acc[c][t][v]));
+                    }
+                }
         };
-        Codes codes[D];
-        load_x();
-#pragma unroll
-        for (int i = 0; i < D - 1; ++i) load_codes(codes[i]);
-        put_x(0);
-        moe::lds_only_barrier();
-        // step i: its x is in LDS; the buffer of step i + 1 was last read in step i - 1
-        int buffer = 0;
-        for (int i = 0; i < n_most; i += D) {
-#pragma unroll
-            for (int u = 0; u < D; ++u) {
-                if (i + u >= n_most) break;
-                load_x();
-                load_codes(codes[(u + D - 1) % D]);
-                __builtin_amdgcn_sched_barrier(0);
-                if (i + u < n) multiply(codes[u], buffer);
-                buffer ^= 1;
-                put_x(buffer);
-                moe::lds_only_barrier();
-            }
+        // (row tiles beyond the last one are zeros, and not stored)
+        if constexpr (TM == 4) {
+            if (tiles <= 2) work(std::integral_constant<int, 2>{});
+            else work(std::integral_constant<int, 4>{});
+        } else {
+            if (tiles <= 1) work(std::integral_constant<int, 1>{});
+            else work(std::integral_constant<int, 2>{});
         }
-        if constexpr (KS > 1) {
-            f32x4* const red = (f32x4*)s_mem;
-            if (ks > 0) {
-#pragma unroll
-                for (int c = 0; c < NC; ++c)
-#pragma unroll
-                    for (int t = 0; t < T; ++t) red[((((ks - 1) * CW + cw) * NC + c) * T + t) * 64 + lane] = acc[c][t];
-            }
-            __syncthreads();
-            if (ks > 0) return;
-#pragma unroll
-            for (int s = 1; s < KS; ++s)
-#pragma unroll
-                for (int c = 0; c < NC; ++c)
-#pragma unroll
-                    for (int t = 0; t < T; ++t) acc[c][t] += red[((((s - 1) * CW + cw) * NC + c) * T + t) * 64 + lane];
-        }
-        // ---- acc[c][t][v]: row 4 * g4 + v of row tile t, column r16 of column tile c
-#pragma unroll
-        for (int t = 0; t < T; ++t)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int r = t * 16 + 4 * g4 + v;
-                if (r >= rows) continue;
-#pragma unroll
-                for (int c = 0; c < NH; ++c) {
-                    const int o = col0 + c * 16 + r16;
-                    // the hidden activation is rounded to bf16 once, as the operand of the second product
-                    if constexpr (PHASE == 1) a.h[(size_t)s_row[r] * a.f + o] = (__bf16)(silu(acc[c][t][v]) * acc[NH + c][t][v]);
-                    else a.y[(size_t)s_io[r] * a.d + o] = (__bf16)(s_gate[r] * acc[c][t][v]);
-                }
-            }
-    };
-    // (row tiles beyond the last one are zeros, and not stored)
-    if constexpr (TM == 4) {
-        if (tiles <= 2) work(std::integral_constant<int, 2>{});
-        else work(std::integral_constant<int, 4>{});
-    } else {
-        if (tiles <= 1) work(std::integral_constant<int, 1>{});
-        else work(std::integral_constant<int, 2>{});
+        if (NC == 4 || a.blocks || rows < ROWS) return;                    // (a full block may be followed by another)
+        __syncthreads();                                                   // s_row and the rest are used again
     }
 }
 
+// row blocks per expert that get a workgroup without a list: for three times the average (an expert with more keeps its workgroups for another block)
+int scanned_blocks(const W4Args& a, int rows) {
+    const int held = std::max(1, std::min(a.E, a.M));
+    return (int)std::min<long long>((a.M - 1) / rows + 1, (3LL * a.M - 1) / ((long long)held * rows) + 1);
+}
 template <int PHASE, int TM, int CW, int KS, int NC, int G, bool ZERO> moe_status launch_tile(const W4Args& a, hipStream_t s) {
     const int cols = (PHASE == 1 ? a.f : a.d) / (CW * 16 * (PHASE == 1 ? NC / 2 : NC));
-    constexpr const char* NAMES[] = {"ffn_w4_small1_kernel", "ffn_w4_small2_kernel", "ffn_w4_middle1_kernel", "ffn_w4_middle2_kernel", "ffn_w4_large1_kernel", "ffn_w4_large2_kernel", "ffn_w4_tall1_kernel", "ffn_w4_tall2_kernel"};
-    moe::LaunchScope k(NAMES[(TM == 2 ? 0 : CW == 2 ? 6 : NC == 2 ? 2 : 4) + PHASE - 1], s);
+    constexpr const char* NAMES[] = {"ffn_w4_small1_kernel", "ffn_w4_small2_kernel", "ffn_w4_middle1_kernel", "ffn_w4_middle2_kernel", "ffn_w4_large1_kernel", "ffn_w4_large2_kernel"};
+    moe::LaunchScope k(NAMES[(TM == 2 ? 0 : NC == 2 ? 2 : 4) + PHASE - 1], s);
     // (the kernel deals rows to dies in groups of eight)
-    const dim3 grid = a.blocks ? dim3((unsigned)cols * (unsigned)((a.most_blocks + 7) / 8 * 8)) : dim3(cols, a.E, (a.M - 1) / (16 * TM) + 1);
+    const dim3 grid = a.blocks ? dim3((unsigned)cols * (unsigned)((a.most_blocks + 7) / 8 * 8)) : dim3(cols, a.E, NC == 4 ? (a.M - 1) / (16 * TM) + 1 : scanned_blocks(a, 16 * TM));
     hipLaunchKernelGGL((ffn_w4_tile_kernel<PHASE, TM, CW, KS, NC, G, ZERO>), grid, dim3(CW * KS * 64), 0, s, a);
     return k.done();
 }
@@ -574,26 +582,27 @@ template <int PHASE, bool XLDS, int G, bool ZERO> moe_status launch_stream(const
 }
 
 // ---- which kernel a phase takes, by estimates (us).  M bounds the rows; how they spread over the experts is not known here.
-// Fitted to 8 shapes (E 1 .. 8, d 256 .. 7168, f 512 .. 14336) with 1 .. 2500 rows in groups of 32, 64 and 128, every phase timed in every way.  Streaming / tiles of
-// 32 x 64 / 64 x 128 / 64 x 256, us, groups of 128, phase 1 + phase 2:
-//   E 1, d 4096, f 14336:   1 row 20+13  19+35  27+75  38+129,  12 rows 25+20  21+35  27+75  38+129,  96 rows -  66+47  42+102  58+198,  400 rows -  235+115  145+105  126+200
-//   E 4, d 7168, f 2048:    1 row 14+14  19+9   39+14  63+21,   24 rows 36+17  24+13  41+16  64+22,   200 rows -  44+28  57+26  97+33,  1000 rows -  159+108  115+51  124+45
-//   E 4, d 2048, f 1408:    1 row 12+7   10+7   14+11  20+16,   200 rows -  20+12  21+16  32+25,  2500 rows -  -  61+33  60+33,  8191 rows -  -  151+83  126+80
+// Fitted to 167 shapes (E 1 .. 32, d 256 .. 7168, f 512 .. 14336, 1 .. 8191 rows, groups of 32, 64 and 128), every phase timed in every way; the choice is within
+// 8 % of the best of them but for 5 shapes (32 experts of 1024 x 512 with 256 rows: 33 against 28).  Streaming / tiles of 32 x 64 / 64 x 128 / 64 x 256, us, groups of
+// 128, phase 1 + phase 2 (the tiles of 64 rows with a list of the rows, whose own launch takes 5 and with more rows up to 10):
+//   E 1, d 4096, f 14336:   1 row 21+14  20+36  26+73  34+115,  12 rows 23+20  19+36  27+74  35+115,  96 rows 218+108  62+45  46+98  53+174,  400 rows -  227+107  150+101  132+175
+//   E 4, d 7168, f 2048:    4 rows 21+14  21+11  38+14  57+18,  24 rows 35+18  24+12  40+15  58+19,   200 rows 143+55  41+29  55+25  89+29,   1000 rows -  148+104  111+51  120+43
+//   E 4, d 2048, f 1408:    1 row 12+11  8+7  13+9  17+13,      200 rows 40+39  15+12  19+14  27+21,  2500 rows -  101+63  58+31  55+31,      8191 rows -  305+182  138+77  114+71
 // (64 x 256 tiles in smaller groups: 2500 rows of the last, groups of 64, 67+36 and 81+40: the scales of more groups do not fit its registers.)
-enum Way { W4_STREAM, W4_SMALL, W4_MIDDLE, W4_LARGE, W4_TALL };
+enum Way { W4_STREAM, W4_SMALL, W4_MIDDLE, W4_LARGE };
 struct TileTimes { int rows, weight_rows, slices; double few, full, shared; };      // a step alone on its compute unit with up to half the rows, with all; its share of a full one
-constexpr TileTimes SMALL_TILE = {32, 64, 2, 0.55, 0.75, 0.60}, MIDDLE_TILE = {64, 128, 1, 0.65, 0.88, 0.70}, LARGE_TILE = {64, 256, 1, 1.05, 1.6, 1.25};
+constexpr TileTimes SMALL_TILE = {32, 64, 2, 0.55, 0.82, 0.55}, MIDDLE_TILE = {64, 128, 1, 0.65, 0.90, 0.69}, LARGE_TILE = {64, 256, 1, 0.92, 1.53, 0.97};
 
 struct Phase { int weight_rows, K; };
 double tile_us(const TileTimes& c, const Phase& p, const W4Args& a, int group, bool planned) {
     const double cus = moe::compute_units(), held = std::max(1, std::min(a.E, a.M)), cols = p.weight_rows / c.weight_rows;
     const double blocks = std::max(held, a.M / (double)c.rows + 0.5 * held), steps = (p.K / W4_STEP + c.slices - 1) / c.slices;
-    const double share = blocks * cols / cus, factor = group == 128 ? 1.0 : group == 64 ? 1.15 : 1.5;
+    const double share = blocks * cols / cus, factor = group == 128 ? 1.0 : group == 64 ? 1.06 : 1.24;
     const double alone = a.M / held > c.rows / 2 ? c.full : c.few;
-    double us = 5.0 + factor * steps * std::max(alone, c.shared * (share <= 2.0 ? std::ceil(share) : share));
+    double us = 3.3 + factor * steps * std::max(alone, c.shared * (share <= 2.0 ? std::ceil(share) : share));
     if (!planned) {
-        us += std::max(0.0, a.E * std::ceil(a.M / (double)c.rows) - blocks) * cols * 0.002;           // workgroups that find no rows
-        us += a.S / 256 * 1.2 * std::max(1.0, share / 2);                                           // the walk over the slices
+        us += std::max(0.0, a.E * (c.weight_rows == 256 ? std::ceil(a.M / (double)c.rows) : scanned_blocks(a, c.rows)) - blocks) * cols * 0.005;           // workgroups that find no rows
+        us += 1.6 + a.S / 256 * 1.2 * std::max(1.0, share / 2);                                     // the walk over the slices
     }
     return us;
 }
@@ -601,7 +610,7 @@ double stream_us(const Phase& p, const W4Args& a, int group) {
     const double held = std::max(1, std::min(a.E, a.M)), passes = std::ceil(std::min<double>(a.M, 3.0 * a.M / held) / 16);      // over the most popular expert's weights
     const double bytes = held * p.weight_rows * (p.K / 2.0) * (1.0 + 4.0 / group);
     const bool room = std::min(a.M, 16) * (p.K * 2 + 16) <= STREAM_X_MOST;
-    return 7.0 + passes * ((bytes / 4.2e6) * (room || a.M <= 4 ? 1.0 : 1.6) + 0.6e-4 * a.M / held * p.K) + a.S / 256 * 1.2;
+    return 11.3 + passes * (bytes / 4.2e6) * (room || a.M <= 4 ? 1.0 : 1.6) + a.S / 256 * 1.2;
 }
 // the best way of a phase, and its time
 double best_way(const Phase& p, const W4Args& a, int group, bool planned, Way& way) {
@@ -623,7 +632,6 @@ template <int PHASE, int G, bool ZERO> moe_status launch_way(Way way, const W4Ar
             return rows * (K * 2 + 16) <= STREAM_X_MOST ? launch_stream<PHASE, true, G, ZERO>(a, rows, s) : launch_stream<PHASE, false, G, ZERO>(a, rows, s);
         }
         case W4_SMALL: return launch_tile<PHASE, 2, 2, 2, 2, G, ZERO>(a, s);
-        case W4_TALL: return launch_tile<PHASE, 4, 2, 2, 2, G, ZERO>(a, s);
         case W4_LARGE:
             if constexpr (G == 128) return launch_tile<PHASE, 4, 4, 1, 4, G, ZERO>(a, s);
         default: return launch_tile<PHASE, 4, 4, 1, 2, G, ZERO>(a, s);
@@ -633,7 +641,7 @@ template <int G, bool ZERO> moe_status both_phases(const W4Args& a, void* plan_a
     const Phase p1 = {2 * a.f, a.d}, p2 = {a.d, a.f};
     Way w1, w2, v1, v2;
     const double scanned = best_way(p1, a, G, false, w1) + best_way(p2, a, G, false, w2);
-    const double planned = best_way(p1, a, G, true, v1) + best_way(p2, a, G, true, v2) + 6.0 + a.M * 5e-4;
+    const double planned = best_way(p1, a, G, true, v1) + best_way(p2, a, G, true, v2) + 4.4 + a.M * 5e-4;
     W4Args p = a;
     if (planned < scanned) {                                               // a launch that lists the rows by expert, for both phases
         moe::RowsPlan plan = {a.offsets, a.S, a.E, a.M, 64, a.row_map, a.row_gate, nullptr, 0, nullptr, nullptr};

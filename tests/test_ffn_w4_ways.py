@@ -8,32 +8,17 @@ from test_ffn_w4 import activations, check, offsets_of, run, weights
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 
-# group, M of M + 3 rows in the schedule, S, E, d, f, rows listed by expert first, kernels of the two products
-WAYS = [
-    (32, 1, 1, 1, 256, 1024, False, "small", "stream"),
-    (128, 1, 1, 8, 1024, 128, False, "stream", "small"),
-    (128, 5, 1000, 2, 1024, 1024, False, "small", "small"),
-    (32, 16, 1, 1, 4096, 128, False, "stream", "middle"),                  # 16 rows of 4096 do not fit LDS
-    (128, 16, 1, 1, 256, 4096, False, "small", "stream"),
-    (64, 33, 1, 2, 256, 4096, False, "middle", "small"),
-    (32, 17, 1, 1, 256, 128, False, "small", "middle"),
-    (128, 200, 1, 8, 256, 512, False, "middle", "small"),
-    (32, 200, 1, 8, 256, 512, False, "middle", "small"),
-    (128, 400, 1, 16, 256, 128, False, "middle", "middle"),
-    (128, 400, 1, 64, 256, 128, False, "middle", "large"),
-    (128, 1000, 1, 16, 256, 512, False, "large", "middle"),
-    (128, 2000, 3, 64, 256, 256, True, "middle", "middle"),
-    (32, 1, 2000, 1, 256, 128, True, "middle", "middle"),
-    (64, 700, 1200, 3, 256, 128, True, "middle", "middle"),
-    (128, 33, 1000, 64, 256, 512, True, "large", "middle"),
-    (128, 200, 1000, 64, 1024, 128, True, "middle", "large"),
-    (128, 3000, 1, 256, 256, 128, True, "large", "large"),
-]
+# group, M of M + 3 rows in the schedule, S, E, d, f: few rows and many, few experts and many, few slices and many
+WAYS = [(32, 1, 1, 1, 256, 1024), (128, 1, 1, 8, 1024, 128), (128, 5, 1000, 2, 1024, 1024), (32, 16, 1, 1, 4096, 128), (128, 16, 1, 1, 256, 4096), (64, 33, 1, 2, 256, 4096),
+        (32, 17, 1, 1, 256, 128), (128, 200, 1, 8, 256, 512), (32, 200, 1, 8, 256, 512), (128, 400, 1, 16, 256, 128), (128, 400, 1, 64, 256, 128), (128, 1000, 1, 16, 256, 512),
+        (128, 2000, 3, 64, 256, 256), (32, 1, 2000, 1, 256, 128), (64, 700, 1200, 3, 256, 128), (128, 33, 1000, 64, 256, 512), (128, 200, 1000, 64, 1024, 128), (128, 3000, 1, 256, 256, 128),
+        (64, 130, 1, 1, 512, 2048), (128, 2500, 1, 2, 512, 1024), (128, 100, 1, 4, 4096, 128), (128, 200, 1, 256, 256, 128), (128, 1, 1, 8, 256, 4096)]
+ran = {}                                                                  # case -> its kernels
 
 
 @pytest.mark.parametrize("zeros", [False, True])
-@pytest.mark.parametrize("group,M,S,E,d,f,listed,first,second", WAYS)
-def test_every_way(lib, group, M, S, E, d, f, listed, first, second, zeros):
+@pytest.mark.parametrize("group,M,S,E,d,f", WAYS)
+def test_every_way(lib, group, M, S, E, d, f, zeros):
     rng = np.random.default_rng(M + S)
     sizes = rng.multinomial(M, rng.dirichlet(np.full(S * E, 0.3)))        # uneven, most groups empty
     off = offsets_of(sizes)
@@ -49,9 +34,17 @@ def test_every_way(lib, group, M, S, E, d, f, listed, first, second, zeros):
     finally:
         lib.moe_kernel_timing_enable(False)
     print(names)
+    ran[group, M, S, E, d, f, zeros] = names
     check_rows(y, x, off, E, w, row_map, row_gate)
-    assert "ffn_w4_%s1_kernel" % first in names and "ffn_w4_%s2_kernel" % second in names, names
-    assert ("ffn_plan_kernel" in names) == listed, names
+
+
+def test_every_way_was_taken():
+    """After the cases above: they have used every kernel for both products, and the list of rows and its absence."""
+    if len(ran) < 2 * len(WAYS):
+        pytest.skip("not all cases were run")
+    names = set().union(*ran.values())
+    assert names >= {"ffn_w4_%s%d_kernel" % (way, phase) for way in ("stream", "small", "middle", "large") for phase in (1, 2)} | {"ffn_plan_kernel"}, names
+    assert any("ffn_plan_kernel" not in n and "ffn_w4_large1_kernel" in n for n in ran.values()) and any("ffn_plan_kernel" not in n and "ffn_w4_middle1_kernel" in n for n in ran.values())
 
 
 def check_rows(y, x, off, E, w, row_map, row_gate):
