@@ -5,7 +5,8 @@
 //
 // All of it is one pass over the rows: a row stays in registers between the two sums over its columns, so z and the stream are read once and
 // out and next written once.  HBM bound; a thread owns 8 consecutive columns per step (16 bytes of bf16).  A row of up to 1024 columns belongs to
-// one wavefront (no barriers, four rows per workgroup), a longer one to a workgroup of 256.
+// one wavefront (no barriers, four rows per workgroup), a longer one to a workgroup.  16381 rows of 7168 in bf16: 167 us, 5.6 TB/s (with 256 threads and four steps a row 184); one row of 4096:
+// 3.1 us, a launch and two trips to memory.
 #include "lanes.hpp"
 #include <algorithm>
 
@@ -158,7 +159,8 @@ struct BackwardArgs {
 //   D = d_out + r2 (d_next w2 - n2 mean(d_next w2 n2)),  d_stream = scale D,  d_w2 = sum_t d_next n2
 //   d_gate = sum_c D n1 w1,  d_z = r1 gate (D w1 - n1 mean(D w1 n1)),  d_w1 = sum_t gate D n1
 // Three sums over the columns of a row meet in one reduction (out^2, d_next w2 out, z^2), the fourth (D w1 z) in a second one.
-// The sums over the tokens stay in registers while a workgroup walks its rows.
+// The sums over the tokens stay in registers while a workgroup walks its rows; four wavefronts per SIMD (without the bound on registers a workgroup of 256 had two or three: 137
+// against 127 us).  8192 rows of 4096 with a float32 stream: 119 us, 5.1 TB/s, and 5 for the sums over the workgroups.
 template <int NT, int NV, bool F32, bool JOIN>
 __global__ __attribute__((amdgpu_waves_per_eu(4))) __launch_bounds__(NT == 64 ? 256 : NT)
 void block_backward_kernel(BackwardArgs a) {
@@ -319,12 +321,15 @@ template <int NT, int NV, bool F32, bool JOIN> moe_status forward(const ForwardA
     return k.done();
 }
 template <bool F32, bool JOIN> moe_status forward_of(const ForwardArgs& a, hipStream_t s) {
+    // 8 columns per thread; two steps of 256 threads where more than a third of 512 would have none (T 8192: d 2304 30 us against 34, d 4096 48 against 47, its float32 stream 80
+    // against 74; T 64, d 4096: 8.6 against 6.5; d 8192: 512 threads 104, 1024 threads 100)
     if (a.d <= 512) return forward<64, 1, F32, JOIN>(a, s);
     if (a.d <= 1024) return forward<64, 2, F32, JOIN>(a, s);
     if (a.d <= 2048) return forward<256, 1, F32, JOIN>(a, s);
-    if (a.d <= 4096) return forward<256, 2, F32, JOIN>(a, s);
-    if (a.d <= 8192) return forward<256, 4, F32, JOIN>(a, s);
-    return forward<256, 8, F32, JOIN>(a, s);
+    if (a.d <= 2736) return forward<256, 2, F32, JOIN>(a, s);
+    if (a.d <= 4096) return forward<512, 1, F32, JOIN>(a, s);
+    if (a.d <= 8192) return forward<1024, 1, F32, JOIN>(a, s);
+    return forward<1024, 2, F32, JOIN>(a, s);
 }
 
 template <int NT, int NV, bool F32, bool JOIN> moe_status backward(BackwardArgs a, float* d_w1, float* d_w2, float* work, hipStream_t s) {
@@ -345,11 +350,14 @@ template <int NT, int NV, bool F32, bool JOIN> moe_status backward(BackwardArgs 
     return k.done();
 }
 template <bool F32, bool JOIN> moe_status backward_of(const BackwardArgs& a, float* d_w1, float* d_w2, float* work, hipStream_t s) {
+    // as in the forward pass; a bf16 stream leaves enough registers for two steps of half the threads, which many rows fill better (T 8192, d 7168: 155 us against 165, in float32
+    // 224 against 216; T 64: 17 against 11)
     if (a.d <= 512) return backward<64, 1, F32, JOIN>(a, d_w1, d_w2, work, s);
     if (a.d <= 1024) return backward<64, 2, F32, JOIN>(a, d_w1, d_w2, work, s);
     if (a.d <= 2048) return backward<256, 1, F32, JOIN>(a, d_w1, d_w2, work, s);
-    if (a.d <= 4096) return backward<256, 2, F32, JOIN>(a, d_w1, d_w2, work, s);
-    if (a.d <= 8192) return backward<512, 2, F32, JOIN>(a, d_w1, d_w2, work, s);
+    if (a.d <= 2736) return backward<256, 2, F32, JOIN>(a, d_w1, d_w2, work, s);
+    if (a.d <= 4096) return backward<512, 1, F32, JOIN>(a, d_w1, d_w2, work, s);
+    if (a.d <= 8192) return F32 || a.T <= 1024 ? backward<1024, 1, F32, JOIN>(a, d_w1, d_w2, work, s) : backward<512, 2, F32, JOIN>(a, d_w1, d_w2, work, s);
     return backward<1024, 2, F32, JOIN>(a, d_w1, d_w2, work, s);
 }
 

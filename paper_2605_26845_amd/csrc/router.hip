@@ -3,7 +3,8 @@
 //
 // LANES neighbouring lanes own a token and VPL neighbouring experts each: the logits are read once with wide loads.  Every lane sorts
 // its experts by (logit, lower index first); the largest head of all lanes is taken topk times, and the lane that held it moves its list up.
-// (More than 8 experts per lane are looked through each time instead: sorting them is a quadratic number of exchanges.)
+// (More than 4 experts per lane are looked through each time instead: sorting them is a quadratic number of exchanges.)
+// Bound by the vector instructions of the choice, with few tokens by its chain: 32771 tokens of 64 experts, top-2, in bf16 7.1 us, 64 tokens of 256, top-8, 4.8 us.
 // Neither the order of the lanes nor any atomic decides a tie: equal logits go to the lower index.
 #include "lanes.hpp"
 #include <algorithm>
@@ -74,6 +75,14 @@ __device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + expf(-
 // exp(x - top), top being at least x; equal infinities are as far apart as equal numbers
 __device__ __forceinline__ float exp_below(float x, float top) { return x == top ? 1.0f : expf(x - top); }
 
+// exp(x) for x <= 0 to 2 steps: x log2(e) in two parts, the hardware's power of two of the first, the second to first order (below 2^-126: zero)
+__device__ __forceinline__ float exp_negative(float x) {
+    const float y = fmaxf(x, -200.0f), t = y * 1.44269504f;
+    const float r = __builtin_fmaf(y, 1.44269504f, -t) + y * 1.9259629e-8f, e = __builtin_amdgcn_exp2f(t);
+    return __builtin_fmaf(e, r * 0.693147182f, e);
+}
+__device__ __forceinline__ float exp_below_fast(float x, float top) { return x == top ? 1.0f : exp_negative(x - top); }
+
 // sigmoid(x) / sigmoid(top) for x <= top, also where both are too small for a float
 __device__ __forceinline__ float sigmoid_ratio(float x, float top) {
     const float ex = expf(-__builtin_fabsf(x)), et = expf(-__builtin_fabsf(top));
@@ -94,7 +103,7 @@ void router_topk_kernel(RouterArgs a) {
         for (int i = 0; i < VPL; ++i) v[i] = -__builtin_inff();
     }
     // this lane's experts in falling order (a sort by exchanges of neighbours keeps equal ones in the order of their index)
-    constexpr bool SORTED = VPL <= 8;
+    constexpr bool SORTED = VPL <= 4;
     unsigned int key[VPL], idx[SORTED ? VPL : 1], head, head_idx;
 #pragma unroll
     for (int i = 0; i < VPL; ++i) key[i] = order_key(v[i]);
@@ -127,7 +136,7 @@ void router_topk_kernel(RouterArgs a) {
     float all = 0.0f;                                                      // sum of exp(logit - top) over all experts
     if (a.score == MOE_ROUTER_SOFTMAX && !a.renormalise) {
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) all += v[i] == -__builtin_inff() ? 0.0f : exp_below(v[i], top);
+        for (int i = 0; i < VPL; ++i) all += v[i] == -__builtin_inff() ? 0.0f : exp_below_fast(v[i], top);
         all = moe::lanes_sum<LANES>(all);
     }
     // lane j % LANES keeps slot j's choice
@@ -180,20 +189,12 @@ void router_topk_kernel(RouterArgs a) {
     }
 }
 
-// exp(x) for x <= 0 to 2 steps: x log2(e) in two parts, the hardware's power of two of the first, the second to first order (below 2^-126: zero)
-__device__ __forceinline__ float exp_negative(float x) {
-    const float y = fmaxf(x, -200.0f), t = y * 1.44269504f;
-    const float r = __builtin_fmaf(y, 1.44269504f, -t) + y * 1.9259629e-8f, e = __builtin_amdgcn_exp2f(t);
-    return __builtin_fmaf(e, r * 0.693147182f, e);
-}
-__device__ __forceinline__ float exp_below_fast(float x, float top) { return x == top ? 1.0f : exp_negative(x - top); }
-
 // LANES lanes per token (topk of them at least), which go through its experts in steps of LANES * VPL.  With G_j = scale d_gate_j over the slots whose expert is in range:
 //   softmax                 d_l[e] = p_e (sum of G_j with id_j = e  -  sum_j G_j p_j)
 //   renormalised (w_j sum to one over the slots)      d_l[id_j] += w_j (1 - sigmoid(l_j) for sigmoid scores, else 1) (G_j - sum_k G_k w_k)
 //   sigmoid                 d_l[id_j] += G_j s_j (1 - s_j)
 // What a slot gives its expert meets the expert's lane in LDS, a row of E floats per token.  Bound by the vector instructions of the exponentials: each is taken once
-// (16384 tokens of 256 experts: with a second one per logit, a wavefront per token and every lane asking every slot 16.5 us).
+// (16384 tokens of 256 experts, top-8: 10.5 us, 3.2 TB/s; with a second one per logit, a wavefront per token and every lane asking every slot 16.5 us).
 template <bool F32, int LANES, int VPL, bool WIDE>
 __global__ __launch_bounds__(ROUTER_THREADS)
 void router_backward_kernel(RouterArgs a) {
@@ -334,11 +335,13 @@ template <bool F32, int LANES, int VPL> moe_status launch_topk(const RouterArgs&
     return k.done();
 }
 template <bool F32> moe_status topk_of(const RouterArgs& a, bool wide, hipStream_t s) {
+    // 16 experts per lane cost the fewest instructions (32768 tokens of 128 experts, top-6: 8 lanes 12.6 us, 16 lanes of 8 experts 20; 16384 of 256, top-8: 16 lanes 14.4, 32 of 8
+    // 26, 64 of 4 21; 8192 of 512: 32 lanes 14, 64 of 8 25), four sorted ones per lane the shortest chain (64 tokens of 256: 4.8 against 7.1, level at some 4000 tokens)
     if (a.E <= 16) return launch_topk<F32, 16, 1>(a, wide, s);
     if (a.E <= 64) return launch_topk<F32, 16, 4>(a, wide, s);
-    if (a.E <= 128) return launch_topk<F32, 16, 8>(a, wide, s);
-    if (a.E <= 256) return launch_topk<F32, 32, 8>(a, wide, s);
-    if (a.E <= 512) return launch_topk<F32, 64, 8>(a, wide, s);
+    if (a.E <= 128) return launch_topk<F32, 8, 16>(a, wide, s);
+    if (a.E <= 256) return a.T < 4096 ? launch_topk<F32, 64, 4>(a, wide, s) : launch_topk<F32, 16, 16>(a, wide, s);
+    if (a.E <= 512) return launch_topk<F32, 32, 16>(a, wide, s);
     if (a.E <= 1024) return launch_topk<F32, 64, 16>(a, wide, s);
     return launch_topk<F32, 64, 64>(a, wide, s);
 }
@@ -353,6 +356,8 @@ template <bool F32, int LANES, int VPL> moe_status launch_backward(const RouterA
     return k.done();
 }
 template <bool F32> moe_status backward_of(const RouterArgs& a, bool wide, hipStream_t s) {
+    // as few lanes per token as its experts and slots leave (32768 tokens of 64 experts: 16 lanes 7.4 us, 64 lanes 16.1; 16384 of 256: 32 lanes of 8 experts 10.5, 64 of 4
+    // 11.1, 16 of 16 13.6)
     if (a.topk <= 16 && a.E <= 64) return launch_backward<F32, 16, 4>(a, wide, s);
     if (a.topk <= 16 && a.E <= 128) return launch_backward<F32, 16, 8>(a, wide, s);
     if (a.E <= 256) return launch_backward<F32, 32, 8>(a, wide, s);
