@@ -126,7 +126,8 @@ extern "C" moe_status moe_combine_topk_sum(const void* y, const int32_t* row_of,
 // HBM bound: d_out is read once, y read and d_y written once.  A workgroup takes a token: its threads hold d_out[t] (8 columns a
 // step) and walk the token's rows, whose loads go out together.  Nearly always a row belongs to one assignment and is written right here.  A row that
 // several assignments name (counted beforehand) is left to the workgroups behind the tokens', which add them up in the order of the assignments, and so
-// is a row that none names, whose gradient is zero.
+// is a row that none names, whose gradient is zero.  8192 tokens to 8 rows of 4096: 228 us, 5.0 TB/s, and 9 for the counts; two steps of 256 threads per row (512 threads of one
+// step: 235; 4 rows in flight per token, 8: 229; d 7168: 217 with 512 threads, 228 with 1024).
 namespace {
 
 constexpr int CBB_MAX_COLUMNS = 16384;
