@@ -46,6 +46,7 @@ EXPORTS = [
 ]
 
 _lib = None
+_torch = None                                                             # set by load()
 
 
 class MoeError(RuntimeError):
@@ -80,14 +81,15 @@ def build(verbose: bool = False) -> str:
 
 def load():
     """Load the shared library (built beforehand by build()); fails loudly if it is absent."""
-    global _lib
+    global _lib, _torch
     if _lib is not None:
         return _lib
     if not os.path.exists(_LIB_PATH):
         raise MoeError("libmoecircuit.so is not built: run `python -c 'import __graft_entry__ as g; g.build()'`")
     # torch ships its own HIP runtime (soname libamdhip64.so.7); importing it first makes the
     # library bind to that one instead of bringing a second runtime into the process
-    import torch  # noqa: F401
+    import torch
+    _torch = torch
     L = ctypes.CDLL(_LIB_PATH)
     vp, ci, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
     L.moe_route_histogram.argtypes = [vp, ci, ci, ci, ci, ci, vp, vp, vp]
@@ -472,12 +474,12 @@ def _operands(what, wanted):
 
 def _on(device, what, call, *args):
     """call(*args, stream) on the current stream of `device`, which is made current for it."""
-    import torch
-    if device == torch.cuda.current_device():
-        rc = call(*args, torch._C._cuda_getCurrentRawStream(device))
+    C = _torch._C                                                          # (the operands are on a GPU: torch has set it up)
+    if device == C._cuda_getDevice():
+        rc = call(*args, C._cuda_getCurrentRawStream(device))
     else:
-        with torch.cuda.device(device):
-            rc = call(*args, torch._C._cuda_getCurrentRawStream(device))
+        with _torch.cuda.device(device):
+            rc = call(*args, C._cuda_getCurrentRawStream(device))
     if rc:
         _check(rc, what)
 
@@ -493,36 +495,33 @@ def _at(t):
 
 
 def _bytes(need, workspace, device_of, what):
-    import torch
     if workspace is None:
-        return torch.empty((max(need, 1),), dtype=torch.uint8, device=device_of.device)
-    if not workspace.is_cuda or not workspace.is_contiguous() or workspace.dtype != torch.uint8 or workspace.get_device() != device_of.get_device():
+        return device_of.new_empty((need or 1,), dtype=_torch.uint8)
+    if not workspace.is_cuda or not workspace.is_contiguous() or workspace.dtype != _torch.uint8 or workspace.get_device() != device_of.get_device():
         raise MoeError("%s: workspace must be a contiguous uint8 tensor on the device of the operands" % what)
     return workspace
 
 
 def moe_block_norm(x, weight, eps: float = 1e-6, out=None):
     """x bf16 or float32 [T][d], weight float32 [d] -> out bf16 [T][d] = x / rms(x) * weight."""
-    import torch
-    what = "moe_block_norm"
+    L, torch, what = load(), _torch, "moe_block_norm"
     T, d = _two(x, what, "x")
     if out is None:
-        out = torch.empty((T, d), dtype=torch.bfloat16, device=x.device)
+        out = torch.empty_like(x, dtype=torch.bfloat16)
     dev = _operands(what, (("x", x, (torch.bfloat16, torch.float32), (T, d)), ("weight", weight, torch.float32, (d,)), ("out", out, torch.bfloat16, (T, d))))
-    _on(dev, what, load().moe_block_norm, x.data_ptr(), int(x.dtype == torch.float32), _at(weight), eps, T, d, out.data_ptr())
+    _on(dev, what, L.moe_block_norm, x.data_ptr(), int(x.dtype == torch.float32), _at(weight), eps, T, d, out.data_ptr())
     return out
 
 
 def moe_block_norm_backward(d_out, x, weight, eps: float = 1e-6, d_stream=None, workspace=None):
     """d_out bf16 [T][d], x and d_stream (or None) bf16 or float32 [T][d], weight float32 [d] -> dict(d_x like x = d_stream + the norm's gradient, d_weight)."""
-    import torch
-    what = "moe_block_norm_backward"
+    L, torch, what = load(), _torch, "moe_block_norm_backward"
     T, d = _two(x, what, "x")
     dev = _operands(what, (("d_out", d_out, torch.bfloat16, (T, d)), ("x", x, (torch.bfloat16, torch.float32), (T, d)), ("weight", weight, torch.float32, (d,)),
                            ("d_stream", d_stream, x.dtype, (T, d))))
     o = dict(d_x=torch.empty_like(x), d_weight=torch.empty_like(weight))
-    workspace = _bytes(int(load().moe_block_backward_workspace_bytes(T, d)), workspace, x, what)
-    _on(dev, what, load().moe_block_norm_backward, _at(d_out), x.data_ptr(), int(x.dtype == torch.float32), _at(weight), _at(d_stream), eps, T, d,
+    workspace = _bytes(L.moe_block_backward_workspace_bytes(T, d), workspace, x, what)
+    _on(dev, what, L.moe_block_norm_backward, _at(d_out), x.data_ptr(), int(x.dtype == torch.float32), _at(weight), _at(d_stream), eps, T, d,
         o["d_x"].data_ptr(), o["d_weight"].data_ptr(), workspace.data_ptr(), workspace.numel())
     return o
 
@@ -530,8 +529,7 @@ def moe_block_norm_backward(d_out, x, weight, eps: float = 1e-6, d_stream=None, 
 def moe_block_join(z, stream, post_weight=None, gate=None, next_weight=None, scale: float = 1.0, eps: float = 1e-6, out=None, next_out=None):
     """z bf16 [T][d] (the block's result), stream bf16 or float32 [T][d], weights float32 [d], gate float32 [T] ->
     (out like stream = scale * stream + gate * norm(z), next bf16 = norm(out) or None without next_weight)."""
-    import torch
-    what = "moe_block_join"
+    L, torch, what = load(), _torch, "moe_block_join"
     T, d = _two(z, what, "z")
     _two(stream, what, "stream")
     if out is None:
@@ -542,7 +540,7 @@ def moe_block_join(z, stream, post_weight=None, gate=None, next_weight=None, sca
     dev = _operands(what, (("z", z, torch.bfloat16, (T, d)), ("stream", stream, stream_types, (T, d)), ("post_weight", post_weight, torch.float32, (d,)),
                            ("gate", gate, torch.float32, (T,)), ("next_weight", next_weight, torch.float32, (d,)), ("out", out, stream.dtype, (T, d)),
                            ("next_out", next_out, torch.bfloat16, (T, d))))
-    _on(dev, what, load().moe_block_join, z.data_ptr(), stream.data_ptr(), int(stream.dtype == torch.float32), _at(post_weight), _at(gate),
+    _on(dev, what, L.moe_block_join, z.data_ptr(), stream.data_ptr(), int(stream.dtype == torch.float32), _at(post_weight), _at(gate),
         _at(next_weight), scale, eps, T, d, out.data_ptr(), _at(next_out))
     return out, next_out
 
@@ -551,8 +549,7 @@ def moe_block_join_backward(d_out, d_next, z, out, post_weight=None, gate=None, 
                             workspace=None):
     """d_out (like out, or None), d_next (bf16, with next_weight), z bf16 and out [T][d] as the forward call took and returned them ->
     dict(d_z, d_stream, d_gate, d_post_weight, d_next_weight); the last three are None where their input is."""
-    import torch
-    what = "moe_block_join_backward"
+    L, torch, what = load(), _torch, "moe_block_join_backward"
     T, d = _two(z, what, "z")
     stream_types = (torch.bfloat16, torch.float32)
     if out is None:
@@ -562,8 +559,8 @@ def moe_block_join_backward(d_out, d_next, z, out, post_weight=None, gate=None, 
                            ("next_weight", next_weight, torch.float32, (d,))))
     like = lambda t: None if t is None else torch.empty_like(t)                              # noqa: E731
     o = dict(d_z=torch.empty_like(z), d_stream=torch.empty_like(out), d_gate=like(gate), d_post_weight=like(post_weight), d_next_weight=like(next_weight))
-    workspace = _bytes(int(load().moe_block_backward_workspace_bytes(T, d)), workspace, z, what)
-    _on(dev, what, load().moe_block_join_backward, _at(d_out), _at(d_next), z.data_ptr(), out.data_ptr(), int(out.dtype == torch.float32),
+    workspace = _bytes(L.moe_block_backward_workspace_bytes(T, d), workspace, z, what)
+    _on(dev, what, L.moe_block_join_backward, _at(d_out), _at(d_next), z.data_ptr(), out.data_ptr(), int(out.dtype == torch.float32),
         _at(post_weight), _at(gate), _at(next_weight), scale, eps, T, d, o["d_z"].data_ptr(), o["d_stream"].data_ptr(), _at(o["d_gate"]),
         _at(o["d_post_weight"]), _at(o["d_next_weight"]), workspace.data_ptr(), workspace.numel())
     return o
@@ -580,24 +577,22 @@ def _score(score, what):
 
 def moe_router_topk(logits, topk: int, score: str = "softmax", renormalise: bool = True, scale: float = 1.0, ids=None, gates=None):
     """logits bf16 or float32 [T][E] -> (ids int32 [T][topk], gates float32 [T][topk]); -inf masks an expert, a slot without expert is (-1, 0)."""
-    import torch
-    what = "moe_router_topk"
+    L, torch, what = load(), _torch, "moe_router_topk"
     T, E = _two(logits, what, "logits")
     if ids is None:
-        ids = torch.empty((T, topk), dtype=torch.int32, device=logits.device)
+        ids = logits.new_empty((T, topk), dtype=torch.int32)
     if gates is None:
-        gates = torch.empty((T, topk), dtype=torch.float32, device=logits.device)
+        gates = logits.new_empty((T, topk), dtype=torch.float32)
     dev = _operands(what, (("logits", logits, (torch.bfloat16, torch.float32), (T, E)), ("ids", ids, torch.int32, (T, topk)), ("gates", gates, torch.float32, (T, topk))))
     sc = _score(score, what)
-    _on(dev, what, load().moe_router_topk, logits.data_ptr(), int(logits.dtype == torch.float32), T, E, topk, sc,
+    _on(dev, what, L.moe_router_topk, logits.data_ptr(), int(logits.dtype == torch.float32), T, E, topk, sc,
         MOE_ROUTER_RENORMALISE if renormalise else 0, scale, ids.data_ptr(), gates.data_ptr())
     return ids, gates
 
 
 def moe_router_topk_backward(d_gates, logits, ids, score: str = "softmax", renormalise: bool = True, scale: float = 1.0, d_logits=None):
     """d_gates float32 [T][topk], logits and ids as the forward call took and returned them -> d_logits [T][E] in the type of the logits."""
-    import torch
-    what = "moe_router_topk_backward"
+    L, torch, what = load(), _torch, "moe_router_topk_backward"
     T, E = _two(logits, what, "logits")
     topk = _two(ids, what, "ids")[1]
     if d_logits is None:
@@ -605,22 +600,21 @@ def moe_router_topk_backward(d_gates, logits, ids, score: str = "softmax", renor
     dev = _operands(what, (("d_gates", d_gates, torch.float32, (T, topk)), ("logits", logits, (torch.bfloat16, torch.float32), (T, E)), ("ids", ids, torch.int32, (T, topk)),
                            ("d_logits", d_logits, logits.dtype, (T, E))))
     sc = _score(score, what)
-    _on(dev, what, load().moe_router_topk_backward, d_gates.data_ptr(), logits.data_ptr(), int(logits.dtype == torch.float32), ids.data_ptr(), T,
+    _on(dev, what, L.moe_router_topk_backward, d_gates.data_ptr(), logits.data_ptr(), int(logits.dtype == torch.float32), ids.data_ptr(), T,
         E, topk, sc, MOE_ROUTER_RENORMALISE if renormalise else 0, scale, d_logits.data_ptr())
     return d_logits
 
 
 def moe_combine_topk_sum_backward(d_out, y, row_of, gate=None, workspace=None):
     """d_out bf16 [T][d], y bf16 [R][d], row_of int32 [T][topk], gate float32 [T][topk] or None -> dict(d_y [R][d], d_gate [T][topk] or None)."""
-    import torch
-    what = "moe_combine_topk_sum_backward"
+    L, torch, what = load(), _torch, "moe_combine_topk_sum_backward"
     T, topk = _two(row_of, what, "row_of")
     R, d = _two(y, what, "y")
     dev = _operands(what, (("d_out", d_out, torch.bfloat16, (T, d)), ("y", y, torch.bfloat16, (R, d)), ("row_of", row_of, torch.int32, (T, topk)),
                            ("gate", gate, torch.float32, (T, topk))))
     o = dict(d_y=torch.empty_like(y), d_gate=None if gate is None else torch.empty_like(gate))
-    workspace = _bytes(int(load().moe_combine_backward_workspace_bytes(R)), workspace, y, what)
-    _on(dev, what, load().moe_combine_topk_sum_backward, _at(d_out), y.data_ptr(), row_of.data_ptr(), _at(gate), T, topk, d, R,
+    workspace = _bytes(L.moe_combine_backward_workspace_bytes(R), workspace, y, what)
+    _on(dev, what, L.moe_combine_topk_sum_backward, _at(d_out), y.data_ptr(), row_of.data_ptr(), _at(gate), T, topk, d, R,
         o["d_y"].data_ptr(), _at(o["d_gate"]), workspace.data_ptr(), workspace.numel())
     return o
 
@@ -634,8 +628,7 @@ def moe_expert_ffn_w4_sliced(x, offsets, S: int, E_loc: int, q_gate, q_up, q_dow
     """x bf16 [M][d]; offsets int32 [S*E_loc+1]; codes uint8 q_gate, q_up [E_loc][f][d/2], q_down [E_loc][d][f/2] (even input in the low four bits); scales bf16
     [E_loc][d/group][f] and [E_loc][f/group][d]; zero points uint8 like the scales, or None (= 8); row_map int32 [M] and row_gate float32 [M]
     (entries behind the schedule's last row are not read) -> y bf16 [M][d]."""
-    import torch
-    what = "moe_expert_ffn_w4_sliced"
+    L, torch, what = load(), _torch, "moe_expert_ffn_w4_sliced"
     M, d = _two(x, what, "x")
     if s_gate is None or s_gate.dim() != 3 or q_gate is None or q_gate.dim() != 3 or s_gate.shape[1] < 1:
         raise MoeError("%s: codes and scales must be tensors of three dimensions" % what)
@@ -653,7 +646,7 @@ def moe_expert_ffn_w4_sliced(x, offsets, S: int, E_loc: int, q_gate, q_up, q_dow
                            ("s_down", s_down, torch.bfloat16, down), ("z_gate", z_gate, torch.uint8, up), ("z_up", z_up, torch.uint8, up),
                            ("z_down", z_down, torch.uint8, down), ("row_map", row_map, torch.int32, (M,)), ("row_gate", row_gate, torch.float32, (M,))))
     workspace = _bytes(moe_ffn_w4_workspace_bytes(M, d, f), workspace, x, what)
-    _on(dev, what, load().moe_expert_ffn_w4_sliced, x.data_ptr(), offsets.data_ptr(), M, S, E_loc, d, f, group, q_gate.data_ptr(), q_up.data_ptr(),
+    _on(dev, what, L.moe_expert_ffn_w4_sliced, x.data_ptr(), offsets.data_ptr(), M, S, E_loc, d, f, group, q_gate.data_ptr(), q_up.data_ptr(),
         q_down.data_ptr(), s_gate.data_ptr(), s_up.data_ptr(), s_down.data_ptr(), _at(z_gate), _at(z_up), _at(z_down), _at(row_map), _at(row_gate),
         y.data_ptr(), workspace.data_ptr(), workspace.numel())
     return y

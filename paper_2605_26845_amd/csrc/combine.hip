@@ -125,7 +125,7 @@ extern "C" moe_status moe_combine_topk_sum(const void* y, const int32_t* row_of,
 // moe_combine_topk_sum_backward: d_y[row_of[t][j]] += gate[t][j] d_out[t], d_gate[t][j] = d_out[t] . y[row_of[t][j]].
 // HBM bound: d_out is read once, y read and d_y written once.  A workgroup takes a token: its threads hold d_out[t] (8 columns a
 // step) and walk the token's rows, whose loads go out together.  Nearly always a row belongs to one assignment and is written right here.  A row that
-// several assignments name (counted beforehand) is left to the workgroups behind the tokens', which add them up in the order of the assignments, and so
+// several assignments name (counted beforehand, in small calls by every workgroup for itself) is left to the workgroups behind the tokens', which add them up in the order of the assignments, and so
 // is a row that none names, whose gradient is zero.  8192 tokens to 8 rows of 4096: 228 us, 5.0 TB/s, and 9 for the counts; two steps of 256 threads per row (512 threads of one
 // step: 235; 4 rows in flight per token, 8: 229; d 7168: 217 with 512 threads, 228 with 1024).
 namespace {
@@ -145,20 +145,16 @@ void combine_count_kernel(const int32_t* __restrict__ row_of, int n, int R, int3
     }
 }
 
-// both for few rows and assignments, in LDS: one launch instead of two
-constexpr int COUNT_ROWS = 16384;
-__global__ __launch_bounds__(1024)
-void combine_count_few_kernel(const int32_t* __restrict__ row_of, int n, int R, int32_t* __restrict__ uses) {
-    __shared__ int32_t s_uses[COUNT_ROWS];
-    for (int r = threadIdx.x; r < R; r += 1024) s_uses[r] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += 1024) {
+// by one workgroup, in its LDS
+template <int THREADS>
+__device__ __forceinline__ void count_rows(const int32_t* __restrict__ row_of, int n, int R, int32_t* s_uses) {
+    for (int i = threadIdx.x; i < n; i += THREADS) {
         const int r = row_of[i];
         if ((unsigned)r < (unsigned)R) atomicAdd(s_uses + r, 1);
     }
-    __syncthreads();
-    for (int r = threadIdx.x; r < R; r += 1024) uses[r] = s_uses[r];
 }
+// Few rows and assignments: every workgroup counts for itself, so that the call is one launch (777 tokens to 2 rows: 10.5 us a call, with a launch for the counts 14.4).
+constexpr int COUNT_ROWS = 4096;
 
 struct CombineBackwardArgs {
     const __bf16 *d_out, *y;
@@ -186,14 +182,14 @@ __device__ __forceinline__ cb_u32x4 cb_scaled(const float (&v)[8], float w) {
 // it finds one after the other (777 tokens to 2 rows of 2048, 1 % unnamed: 10 us, with 256 rows per workgroup 21 us; 65536 rows of 4096 looked at one by one: 28 us more).
 // The several are found by going through all assignments, a workgroup's width at a time, and added in their order.
 template <int THREADS>
-__device__ __forceinline__ void combine_backward_rest(const CombineBackwardArgs& a, int first, int step) {
+__device__ __forceinline__ void combine_backward_rest(const CombineBackwardArgs& a, const int32_t* uses_of, int first, int step) {
     constexpr int W = THREADS / 64;
     __shared__ unsigned long long s_hit[W], s_odd[W];
     const int wave = threadIdx.x >> 6;
     const long long n = (long long)a.T * a.topk;
     const int share = min(THREADS, (a.R - 1) / step + 1);
     for (long long r0 = (long long)first * share; r0 < a.R; r0 += (long long)step * share) {
-        const unsigned long long odd = __ballot((int)threadIdx.x < share && r0 + threadIdx.x < a.R && a.uses[r0 + threadIdx.x] != 1);
+        const unsigned long long odd = __ballot((int)threadIdx.x < share && r0 + threadIdx.x < a.R && uses_of[r0 + threadIdx.x] != 1);
         __syncthreads();
         if ((threadIdx.x & 63) == 0) s_odd[wave] = odd;
         __syncthreads();
@@ -201,7 +197,7 @@ __device__ __forceinline__ void combine_backward_rest(const CombineBackwardArgs&
             if (s_odd[q >> 6] == 0) { q |= 63; continue; }
             if (!((s_odd[q >> 6] >> (q & 63)) & 1)) continue;
             const long long r = r0 + q;
-            const int uses = a.uses[r];                                        // (the same for the whole workgroup)
+            const int uses = uses_of[r];                                        // (the same for the whole workgroup)
             if (uses == 0) {
                 for (int col = threadIdx.x * 8; col < a.d; col += THREADS * 8) *reinterpret_cast<cb_u32x4*>(a.d_y + (size_t)r * a.d + col) = cb_u32x4{0u, 0u, 0u, 0u};
                 continue;
@@ -240,17 +236,27 @@ __device__ __forceinline__ void combine_backward_rest(const CombineBackwardArgs&
     }
 }
 
-// NT threads per token, NV steps of NT * 8 columns, J rows of y in flight at once
-template <int NT, int NV, int J>
+// NT threads per token, NV steps of NT * 8 columns, J rows of y in flight at once; COUNT: the rows' counts are made here, in LDS (R integers)
+template <int NT, int NV, int J, bool COUNT>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT)
 void combine_backward_kernel(CombineBackwardArgs a) {
     constexpr int PER = NT == 64 ? 4 : 1;
     __shared__ float s_sum[2 * J * (NT / 64)];
+    extern __shared__ int32_t s_uses[];
+    const int32_t* uses = a.uses;
+    if constexpr (COUNT) {
+        constexpr int THREADS = NT == 64 ? 256 : NT;
+        for (int r = threadIdx.x; r < a.R; r += THREADS) s_uses[r] = 0;
+        __syncthreads();
+        count_rows<THREADS>(a.row_of, a.T * a.topk, a.R, s_uses);
+        __syncthreads();
+        uses = s_uses;
+    }
     int half = 0;
     const int tid = threadIdx.x % NT;
     const int token_blocks = a.T == 0 ? 0 : (a.T - 1) / PER + 1;
     if ((int)blockIdx.x >= token_blocks) {                                // the workgroups behind the tokens'
-        combine_backward_rest<(NT == 64 ? 256 : NT)>(a, (int)blockIdx.x - token_blocks, (int)gridDim.x - token_blocks);
+        combine_backward_rest<(NT == 64 ? 256 : NT)>(a, uses, (int)blockIdx.x - token_blocks, (int)gridDim.x - token_blocks);
         return;
     }
     const long long t = (long long)blockIdx.x * PER + (int)threadIdx.x / NT;
@@ -273,7 +279,7 @@ void combine_backward_kernel(CombineBackwardArgs a) {
             row[j] = j0 + j < a.topk ? a.row_of[at] : -1;
             if ((unsigned)row[j] >= (unsigned)a.R) row[j] = -1;
             w[j] = a.gate && row[j] >= 0 ? a.gate[at] : 1.0f;
-            alone[j] = row[j] >= 0 && a.uses[row[j]] == 1;
+            alone[j] = row[j] >= 0 && uses[row[j]] == 1;
             dot[j] = 0.0f;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
@@ -309,15 +315,17 @@ void combine_backward_kernel(CombineBackwardArgs a) {
     }
 }
 
-template <int NT, int NV, int J> void launch_combine_backward(const CombineBackwardArgs& a, hipStream_t s) {
+template <int NT, int NV, int J> void launch_combine_backward(const CombineBackwardArgs& a, bool count, hipStream_t s) {
     constexpr int PER = NT == 64 ? 4 : 1;
     const int token_blocks = a.T == 0 ? 0 : (a.T - 1) / PER + 1, rest_blocks = std::min(a.R, moe::compute_units());
-    hipLaunchKernelGGL((combine_backward_kernel<NT, NV, J>), dim3((unsigned)token_blocks + (unsigned)rest_blocks), dim3(NT == 64 ? 256 : NT), 0, s, a);
+    const dim3 grid((unsigned)token_blocks + (unsigned)rest_blocks), block(NT == 64 ? 256 : NT);
+    if (count) hipLaunchKernelGGL((combine_backward_kernel<NT, NV, J, true>), grid, block, a.R * (int)sizeof(int32_t), s, a);
+    else hipLaunchKernelGGL((combine_backward_kernel<NT, NV, J, false>), grid, block, 0, s, a);
 }
-template <int NT, int NV> void launch_combine_backward(const CombineBackwardArgs& a, hipStream_t s) {
-    if (a.topk == 1) launch_combine_backward<NT, NV, 1>(a, s);
-    else if (a.topk == 2) launch_combine_backward<NT, NV, 2>(a, s);
-    else launch_combine_backward<NT, NV, 4>(a, s);
+template <int NT, int NV> void launch_combine_backward(const CombineBackwardArgs& a, bool count, hipStream_t s) {
+    if (a.topk == 1) launch_combine_backward<NT, NV, 1>(a, count, s);
+    else if (a.topk == 2) launch_combine_backward<NT, NV, 2>(a, count, s);
+    else launch_combine_backward<NT, NV, 4>(a, count, s);
 }
 
 }  // namespace
@@ -335,24 +343,21 @@ extern "C" moe_status moe_combine_topk_sum_backward(const void* d_out, const voi
     const int cus = moe::compute_units(), n = T * topk;
     CombineBackwardArgs a = {(const __bf16*)d_out, (const __bf16*)y, row_of, gate, (const int32_t*)workspace, (__bf16*)d_y, d_gate, T, topk, d, R};
     const auto blocks = [&](int items) { return dim3((unsigned)std::min((items - 1) / 256 + 1, cus * 8)); };
-    if (R > 0) {
+    const bool count_here = R <= COUNT_ROWS && n <= COUNT_ROWS;
+    if (R > 0 && !count_here) {
         moe::LaunchScope k("combine_count_kernel", s);
-        if (R <= COUNT_ROWS && n <= COUNT_ROWS) {
-            hipLaunchKernelGGL(combine_count_few_kernel, dim3(1), dim3(1024), 0, s, row_of, n, R, (int32_t*)workspace);
-        } else {
-            hipLaunchKernelGGL(combine_clear_kernel, blocks(R), dim3(256), 0, s, (int32_t*)workspace, R);
-            if (n > 0) hipLaunchKernelGGL(combine_count_kernel, blocks(n), dim3(256), 0, s, row_of, n, R, (int32_t*)workspace);
-        }
+        hipLaunchKernelGGL(combine_clear_kernel, blocks(R), dim3(256), 0, s, (int32_t*)workspace, R);
+        if (n > 0) hipLaunchKernelGGL(combine_count_kernel, blocks(n), dim3(256), 0, s, row_of, n, R, (int32_t*)workspace);
         if (const moe_status st = k.done()) return st;
     }
     if (T > 0 || R > 0) {
         moe::LaunchScope k("combine_backward_kernel", s);
-        if (d <= 512) launch_combine_backward<64, 1>(a, s);
-        else if (d <= 1024) launch_combine_backward<64, 2>(a, s);
-        else if (d <= 2048) launch_combine_backward<256, 1>(a, s);
-        else if (d <= 4096) launch_combine_backward<256, 2>(a, s);
-        else if (d <= 8192) launch_combine_backward<512, 2>(a, s);
-        else launch_combine_backward<1024, 2>(a, s);
+        if (d <= 512) launch_combine_backward<64, 1>(a, count_here, s);
+        else if (d <= 1024) launch_combine_backward<64, 2>(a, count_here, s);
+        else if (d <= 2048) launch_combine_backward<256, 1>(a, count_here, s);
+        else if (d <= 4096) launch_combine_backward<256, 2>(a, count_here, s);
+        else if (d <= 8192) launch_combine_backward<512, 2>(a, count_here, s);
+        else launch_combine_backward<1024, 2>(a, count_here, s);
         if (const moe_status st = k.done()) return st;
     }
     return MOE_OK;

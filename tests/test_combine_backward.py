@@ -117,3 +117,15 @@ def test_edges_and_refused_tensors(lib):
                 lambda: lib.moe_combine_topk_sum_backward(x[:2], y, r, g)):
         with pytest.raises(lib.MoeError):
             bad()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,R", [(2000, 7000), (1366, 4096), (1365, 4097), (1365, 4096), (40, 9000)])
+def test_many_rows_with_odd_ones(lib, T, R):
+    """Both ways of counting the rows' uses, at their boundary too: rows that nothing names, rows named twice and rows named by many."""
+    d_out, y, row_of, gate = _case(T, 3, 72, R, T + R, True)
+    row_of[::7, 1] = row_of[::7, 0]
+    row_of[5::11, 2] = R - 1
+    row_of[3::13, 0] = -1
+    _check(lib, d_out, y, row_of, gate)
+    _check(lib, d_out, y, row_of, None)
