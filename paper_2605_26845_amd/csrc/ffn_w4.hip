@@ -303,14 +303,18 @@ void ffn_w4_stream_kernel(W4Args a, int x_rows) {
 
 // ---------------------------------------------------------------------------------- more rows per expert
 // A workgroup takes up to 16 * TM rows of one expert and CW * NC * 16 weight rows; a wavefront NC tiles of 16 weight rows and all the rows, so
-// that a code is widened once for up to 16 * TM rows.  The codes come straight from memory into registers, D - 1 steps of K = 128 ahead.  x goes
-// through LDS (three buffers; chunks of 16 bytes at place chunk ^ (row % 16) of a row, so that the 16 rows of a fragment lie in different
-// banks); the CW wavefronts that share it take the group sums of x of the next step in turns, a product with a constant.  KS slices of wavefronts share the
-// contraction and add their sums in LDS at the end.
-// With few workgroups bound by a step's chain (fragments from LDS, widening, products, barrier: 0.55 to 1.6 us by the size of a tile), with many by the vector
-// instructions beside the matrix ones (widening 2 per pair of codes, with zero points 3, and a multiply-add per sum and group) and by LDS: 8191 rows of E 4, d 2048, f 1408, groups of 128,
-// in tiles of 64 x 256: 126 and 80 us, 750 and 590 TFLOP/s, matrix cores busy a third of the time; groups of 32 with zero points, in tiles of 64 x 128, 216 and 117.
-// Tiles of 128 x 256 (one wavefront per SIMD, whose sums spill to the matrix cores' half of the registers and are copied for every multiply-add): 196 and 110.
+// that a code is widened once for up to 16 * TM rows.  The codes come straight from memory into registers, a step of K = 128 ahead.  x goes
+// through LDS (two buffers; chunks of 16 bytes at place chunk ^ (row % 16) of a row, so that the 16 rows of a fragment lie in different
+// banks).  KS slices of wavefronts share the contraction and add their sums in LDS at the end.
+// Bound by issue: 4000 rows of d and f 4096, groups of 128, tiles of 64 x 256: 305 + 158 us (880 and 850 TFLOP/s), the matrix cores busy 52 % of the cycles (a fifth of it for the groups'
+// sums of x), the vector instructions (widening 2 per pair of codes, with zero points 3, and a multiply-add per sum and group) 39 %, and little of both at once.  8191 rows of
+// E 4, d 2048, f 1408: 114 and 71 us; groups of 32 with zero points, in tiles of 64 x 128, 188 and 104.  203 rows of E 4, d 7168, f 2048, groups of 32 with zero points, in tiles of
+// 32 x 64: 54 and 37 us, vector instructions 56 % of the cycles; without loading x 47 + 29, without loading codes 48 + 30.
+// Two workgroups per compute unit, not three, though smaller tiles leave registers for it: the dispatcher then loads some compute units with three and others with
+// one (54 us above becomes 66).  Measured without a gain: codes or x further ahead; four slices; the sums of x through LDS, a step ahead (117 and 75 us at 8191 rows, 61 and 36 at 203); column
+// tile by column tile, the codes of the next one widened between the products of this one (117 and 71); starting column tiles at different steps; h step by step in
+// memory; a raised priority for the products.  Tiles of 128 x 256 (one wavefront per SIMD, whose sums spill to the matrix cores' half of the registers and are copied for
+// every multiply-add): 196 and 110.
 template <int PHASE, int TM, int CW, int KS, int NC, int G, bool ZERO>
 __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(CW * KS * 64)
 void ffn_w4_tile_kernel(W4Args a) {
