@@ -68,6 +68,7 @@ struct ForwardArgs {
     void *out, *next;                          // out: join only
     float scale, eps;
     int T, d;
+    int first;                                 // row of the first workgroup
 };
 
 // NT threads and NV steps of NT * 8 columns per row
@@ -78,7 +79,7 @@ void block_forward_kernel(ForwardArgs a) {
     __shared__ float s_sum[2 * (NT / 64)];
     int half = 0;
     const int tid = threadIdx.x % NT;
-    const int row = blockIdx.x * PER + (int)threadIdx.x / NT;
+    const long long row = a.first + (long long)blockIdx.x * PER + (int)threadIdx.x / NT;
     if (row >= a.T) return;                                               // (a whole wavefront, which meets no barrier if NT is 64)
     const size_t base = (size_t)row * a.d;
     Raw8 rz[NV], rx[NV];
@@ -314,10 +315,15 @@ void block_columns_kernel(const float* part_a, float* out_a, const float* part_b
     }
 }
 
-template <int NT, int NV, bool F32, bool JOIN> moe_status forward(const ForwardArgs& a, hipStream_t s) {
+constexpr int MOST_ROWS = 1 << 21;               // per launch, whose threads are counted in 32 bits
+template <int NT, int NV, bool F32, bool JOIN> moe_status forward(ForwardArgs a, hipStream_t s) {
     constexpr int PER = NT == 64 ? 4 : 1;
     moe::LaunchScope k(JOIN ? "block_join_kernel" : "block_norm_kernel", s);
-    hipLaunchKernelGGL((block_forward_kernel<NT, NV, F32, JOIN>), dim3((unsigned)((a.T - 1) / PER + 1)), dim3(NT == 64 ? 256 : NT), 0, s, a);
+    for (long long first = 0; first < a.T; first += MOST_ROWS) {
+        a.first = (int)first;
+        const int rows = (int)std::min<long long>(a.T - first, MOST_ROWS);
+        hipLaunchKernelGGL((block_forward_kernel<NT, NV, F32, JOIN>), dim3((unsigned)((rows - 1) / PER + 1)), dim3(NT == 64 ? 256 : NT), 0, s, a);
+    }
     return k.done();
 }
 template <bool F32, bool JOIN> moe_status forward_of(const ForwardArgs& a, hipStream_t s) {
@@ -385,7 +391,7 @@ extern "C" moe_status moe_block_norm(const void* x, int stream_type, const float
     if (const moe_status st = checked(T, d, stream_type, 1.0f, eps)) return st;
     if (T == 0) return MOE_OK;
     if (!x || !weight || !out || misaligned({x, weight, out})) return MOE_ERR_INVALID_ARG;
-    const ForwardArgs a = {nullptr, x, nullptr, nullptr, weight, nullptr, out, 1.0f, eps, T, d};
+    const ForwardArgs a = {nullptr, x, nullptr, nullptr, weight, nullptr, out, 1.0f, eps, T, d, 0};
     return stream_type == MOE_T_F32 ? forward_of<true, false>(a, (hipStream_t)hip_stream) : forward_of<false, false>(a, (hipStream_t)hip_stream);
 }
 
@@ -395,7 +401,7 @@ extern "C" moe_status moe_block_join(const void* z, const void* stream, int stre
     if ((next_weight == nullptr) != (next == nullptr) && T > 0) return MOE_ERR_INVALID_ARG;
     if (T == 0) return MOE_OK;
     if (!z || !stream || !out || misaligned({z, stream, post_weight, next_weight, out, next})) return MOE_ERR_INVALID_ARG;
-    const ForwardArgs a = {z, stream, post_weight, gate, next_weight, out, next, scale, eps, T, d};
+    const ForwardArgs a = {z, stream, post_weight, gate, next_weight, out, next, scale, eps, T, d, 0};
     return stream_type == MOE_T_F32 ? forward_of<true, true>(a, (hipStream_t)hip_stream) : forward_of<false, true>(a, (hipStream_t)hip_stream);
 }
 

@@ -164,6 +164,7 @@ struct CombineBackwardArgs {
     __bf16* d_y;
     float* d_gate;
     int T, topk, d, R;
+    int first, tokens;                         // of this launch
 };
 
 __device__ __forceinline__ void cb_widen(cb_u32x4 r, float (&v)[8]) {
@@ -254,12 +255,12 @@ void combine_backward_kernel(CombineBackwardArgs a) {
     }
     int half = 0;
     const int tid = threadIdx.x % NT;
-    const int token_blocks = a.T == 0 ? 0 : (a.T - 1) / PER + 1;
+    const int token_blocks = a.tokens == 0 ? 0 : (a.tokens - 1) / PER + 1;
     if ((int)blockIdx.x >= token_blocks) {                                // the workgroups behind the tokens'
         combine_backward_rest<(NT == 64 ? 256 : NT)>(a, uses, (int)blockIdx.x - token_blocks, (int)gridDim.x - token_blocks);
         return;
     }
-    const long long t = (long long)blockIdx.x * PER + (int)threadIdx.x / NT;
+    const long long t = a.first + (long long)blockIdx.x * PER + (int)threadIdx.x / NT;
     if (t >= a.T) return;                                                 // (a whole wavefront, which meets no barrier if NT is 64)
     cb_u32x4 raw[NV];
 #pragma unroll
@@ -315,12 +316,19 @@ void combine_backward_kernel(CombineBackwardArgs a) {
     }
 }
 
-template <int NT, int NV, int J> void launch_combine_backward(const CombineBackwardArgs& a, bool count, hipStream_t s) {
+constexpr int MOST_TOKENS = 1 << 21;              // per launch, whose threads are counted in 32 bits
+template <int NT, int NV, int J> void launch_combine_backward(CombineBackwardArgs a, bool count, hipStream_t s) {
     constexpr int PER = NT == 64 ? 4 : 1;
-    const int token_blocks = a.T == 0 ? 0 : (a.T - 1) / PER + 1, rest_blocks = std::min(a.R, moe::compute_units());
-    const dim3 grid((unsigned)token_blocks + (unsigned)rest_blocks), block(NT == 64 ? 256 : NT);
-    if (count) hipLaunchKernelGGL((combine_backward_kernel<NT, NV, J, true>), grid, block, a.R * (int)sizeof(int32_t), s, a);
-    else hipLaunchKernelGGL((combine_backward_kernel<NT, NV, J, false>), grid, block, 0, s, a);
+    long long first = 0;
+    do {
+        a.first = (int)first;
+        a.tokens = (int)std::min<long long>(a.T - first, MOST_TOKENS);
+        const int token_blocks = a.tokens == 0 ? 0 : (a.tokens - 1) / PER + 1, rest_blocks = first + a.tokens == a.T ? std::min(a.R, moe::compute_units()) : 0;
+        const dim3 grid((unsigned)token_blocks + (unsigned)rest_blocks), block(NT == 64 ? 256 : NT);
+        if (count) hipLaunchKernelGGL((combine_backward_kernel<NT, NV, J, true>), grid, block, a.R * (int)sizeof(int32_t), s, a);
+        else hipLaunchKernelGGL((combine_backward_kernel<NT, NV, J, false>), grid, block, 0, s, a);
+        first += MOST_TOKENS;
+    } while (first < a.T);
 }
 template <int NT, int NV> void launch_combine_backward(const CombineBackwardArgs& a, bool count, hipStream_t s) {
     if (a.topk == 1) launch_combine_backward<NT, NV, 1>(a, count, s);
@@ -341,7 +349,7 @@ extern "C" moe_status moe_combine_topk_sum_backward(const void* d_out, const voi
     if (R > 0 && (!workspace || workspace_bytes < moe_combine_backward_workspace_bytes(R))) return MOE_ERR_WORKSPACE;
     hipStream_t s = (hipStream_t)hip_stream;
     const int cus = moe::compute_units(), n = T * topk;
-    CombineBackwardArgs a = {(const __bf16*)d_out, (const __bf16*)y, row_of, gate, (const int32_t*)workspace, (__bf16*)d_y, d_gate, T, topk, d, R};
+    CombineBackwardArgs a = {(const __bf16*)d_out, (const __bf16*)y, row_of, gate, (const int32_t*)workspace, (__bf16*)d_y, d_gate, T, topk, d, R, 0, 0};
     const auto blocks = [&](int items) { return dim3((unsigned)std::min((items - 1) / 256 + 1, cus * 8)); };
     const bool count_here = R <= COUNT_ROWS && n <= COUNT_ROWS;
     if (R > 0 && !count_here) {

@@ -547,9 +547,10 @@ void ffn_w4_tile_kernel(W4Args a) {
 }
 
 // row blocks per expert that get a workgroup without a list: for three times the average (an expert with more keeps its workgroups for another block)
+constexpr long long MOST_BLOCKS = 65535;          // of a grid's third dimension
 int scanned_blocks(const W4Args& a, int rows) {
     const int held = std::max(1, std::min(a.E, a.M));
-    return (int)std::min<long long>((a.M - 1) / rows + 1, (3LL * a.M - 1) / ((long long)held * rows) + 1);
+    return (int)std::min<long long>({(a.M - 1) / rows + 1, (3LL * a.M - 1) / ((long long)held * rows) + 1, MOST_BLOCKS});
 }
 template <int PHASE, int TM, int CW, int KS, int NC, int G, bool ZERO> moe_status launch_tile(const W4Args& a, hipStream_t s) {
     const int cols = (PHASE == 1 ? a.f : a.d) / (CW * 16 * (PHASE == 1 ? NC / 2 : NC));
@@ -625,7 +626,7 @@ double best_way(const Phase& p, const W4Args& a, int group, bool planned, Way& w
         consider(W4_SMALL, tile_us(SMALL_TILE, p, a, group, planned));
     }
     consider(W4_MIDDLE, tile_us(MIDDLE_TILE, p, a, group, planned));
-    if (group == 128) consider(W4_LARGE, tile_us(LARGE_TILE, p, a, group, planned));
+    if (group == 128 && (planned || (a.M - 1) / LARGE_TILE.rows < MOST_BLOCKS)) consider(W4_LARGE, tile_us(LARGE_TILE, p, a, group, planned));
     return least;
 }
 

@@ -25,6 +25,7 @@ struct RouterArgs {
     void* d_logits;
     float scale;
     int T, E, topk, score, renormalise;
+    int first;                                 // token of the first workgroup
 };
 
 // the first expert of this lane is e0; experts past the end and NaN count as masked
@@ -93,7 +94,7 @@ template <bool F32, int LANES, int VPL, bool WIDE>
 __global__ __launch_bounds__(ROUTER_THREADS)
 void router_topk_kernel(RouterArgs a) {
     const int sub = threadIdx.x % LANES;
-    const long long t = (long long)blockIdx.x * (ROUTER_THREADS / LANES) + threadIdx.x / LANES;
+    const long long t = a.first + (long long)blockIdx.x * (ROUTER_THREADS / LANES) + threadIdx.x / LANES;
     const bool live = t < a.T;                                             // (lanes of other tokens take part in the wavefront's exchanges)
     const int e0 = sub * VPL;
     float v[VPL];
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(ROUTER_THREADS)
 void router_backward_kernel(RouterArgs a) {
     extern __shared__ __attribute__((aligned(16))) float s_give[];
     const int sub = threadIdx.x % LANES;
-    const long long t = (long long)blockIdx.x * (ROUTER_THREADS / LANES) + threadIdx.x / LANES;
+    const long long t = a.first + (long long)blockIdx.x * (ROUTER_THREADS / LANES) + threadIdx.x / LANES;
     const bool live = t < a.T;                                             // (lanes of other tokens take part in the wavefront's exchanges)
     const size_t row = live ? (size_t)t * a.E : 0;
     const int pitch = (a.E + 3) & ~3;                                      // (16 bytes)
@@ -326,12 +327,16 @@ void router_backward_kernel(RouterArgs a) {
     }
 }
 
-template <bool F32, int LANES, int VPL> moe_status launch_topk(const RouterArgs& a, bool wide, hipStream_t s) {
+constexpr int MOST_TOKENS = 1 << 24;              // per launch, whose threads are counted in 32 bits
+template <bool F32, int LANES, int VPL> moe_status launch_topk(RouterArgs a, bool wide, hipStream_t s) {
     constexpr int PER = ROUTER_THREADS / LANES;
     moe::LaunchScope k("router_topk_kernel", s);
-    const dim3 grid((unsigned)((a.T - 1) / PER + 1)), block(ROUTER_THREADS);
-    if (wide) hipLaunchKernelGGL((router_topk_kernel<F32, LANES, VPL, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((router_topk_kernel<F32, LANES, VPL, false>), grid, block, 0, s, a);
+    for (long long first = 0; first < a.T; first += MOST_TOKENS) {
+        a.first = (int)first;
+        const dim3 grid((unsigned)((std::min<long long>(a.T - first, MOST_TOKENS) - 1) / PER + 1)), block(ROUTER_THREADS);
+        if (wide) hipLaunchKernelGGL((router_topk_kernel<F32, LANES, VPL, true>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((router_topk_kernel<F32, LANES, VPL, false>), grid, block, 0, s, a);
+    }
     return k.done();
 }
 template <bool F32> moe_status topk_of(const RouterArgs& a, bool wide, hipStream_t s) {
@@ -346,13 +351,16 @@ template <bool F32> moe_status topk_of(const RouterArgs& a, bool wide, hipStream
     return launch_topk<F32, 64, 64>(a, wide, s);
 }
 
-template <bool F32, int LANES, int VPL> moe_status launch_backward(const RouterArgs& a, bool wide, hipStream_t s) {
+template <bool F32, int LANES, int VPL> moe_status launch_backward(RouterArgs a, bool wide, hipStream_t s) {
     constexpr int PER = ROUTER_THREADS / LANES;
     moe::LaunchScope k("router_backward_kernel", s);
-    const dim3 grid((unsigned)((a.T - 1) / PER + 1)), block(ROUTER_THREADS);
     const int lds = PER * ((a.E + 3) & ~3) * (int)sizeof(float);           // (64 KiB for the most experts)
-    if (wide) hipLaunchKernelGGL((router_backward_kernel<F32, LANES, VPL, true>), grid, block, lds, s, a);
-    else hipLaunchKernelGGL((router_backward_kernel<F32, LANES, VPL, false>), grid, block, lds, s, a);
+    for (long long first = 0; first < a.T; first += MOST_TOKENS) {
+        a.first = (int)first;
+        const dim3 grid((unsigned)((std::min<long long>(a.T - first, MOST_TOKENS) - 1) / PER + 1)), block(ROUTER_THREADS);
+        if (wide) hipLaunchKernelGGL((router_backward_kernel<F32, LANES, VPL, true>), grid, block, lds, s, a);
+        else hipLaunchKernelGGL((router_backward_kernel<F32, LANES, VPL, false>), grid, block, lds, s, a);
+    }
     return k.done();
 }
 template <bool F32> moe_status backward_of(const RouterArgs& a, bool wide, hipStream_t s) {
@@ -379,7 +387,7 @@ extern "C" moe_status moe_router_topk(const void* logits, int logits_type, int T
     if (T == 0) return MOE_OK;
     const bool f32 = logits_type == MOE_T_F32;
     if (!logits || !ids || !gates || ((uintptr_t)logits & (f32 ? 3 : 1)) != 0 || (((uintptr_t)ids | (uintptr_t)gates) & 3) != 0) return MOE_ERR_INVALID_ARG;
-    const RouterArgs a = {logits, nullptr, nullptr, ids, gates, nullptr, scale, T, E, topk, score, flags & MOE_ROUTER_RENORMALISE};
+    const RouterArgs a = {logits, nullptr, nullptr, ids, gates, nullptr, scale, T, E, topk, score, flags & MOE_ROUTER_RENORMALISE, 0};
     // rows start on 16 bytes: pieces of 16 bytes, else one value at a time
     const bool wide = ((uintptr_t)logits & 15) == 0 && E % (f32 ? 4 : 8) == 0;
     return f32 ? topk_of<true>(a, wide, (hipStream_t)hip_stream) : topk_of<false>(a, wide, (hipStream_t)hip_stream);
@@ -391,7 +399,7 @@ extern "C" moe_status moe_router_topk_backward(const float* d_gates, const void*
     if (T == 0) return MOE_OK;
     const bool f32 = logits_type == MOE_T_F32;
     if (!d_gates || !logits || !ids || !d_logits || ((((uintptr_t)logits | (uintptr_t)d_logits) & (f32 ? 3 : 1)) != 0) || (((uintptr_t)ids | (uintptr_t)d_gates) & 3) != 0) return MOE_ERR_INVALID_ARG;
-    const RouterArgs a = {logits, ids, d_gates, nullptr, nullptr, d_logits, scale, T, E, topk, score, flags & MOE_ROUTER_RENORMALISE};
+    const RouterArgs a = {logits, ids, d_gates, nullptr, nullptr, d_logits, scale, T, E, topk, score, flags & MOE_ROUTER_RENORMALISE, 0};
     const bool wide = (((uintptr_t)logits | (uintptr_t)d_logits) & 15) == 0 && E % (f32 ? 4 : 8) == 0;
     hipStream_t s = (hipStream_t)hip_stream;
     return f32 ? backward_of<true>(a, wide, s) : backward_of<false>(a, wide, s);

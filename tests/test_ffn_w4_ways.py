@@ -74,3 +74,34 @@ def test_rows_behind_two_gib(lib, M, d, f, zeros):
     assert not y[: M - last].any().item()
     one = {k: (None if v is None else v[1:]) for k, v in w.items()}
     check(y[M - last:], tail, offsets_of([last]), 1, one)
+
+
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("E,M,e,S", [(8, 200, 3, 1), (64, 300, 63, 5), (8, 41, 0, 1), (4, 2000, 1, 2)])
+def test_all_rows_with_one_expert(lib, E, M, e, S, group):
+    """An expert with many times the average has more row blocks than its grid has: workgroups take another one."""
+    sizes = np.zeros(S * E, dtype=int)
+    sizes[e::E] = np.random.default_rng(M).multinomial(M, np.full(S, 1.0 / S))
+    off = offsets_of(sizes)
+    x, w = activations(M, 512, M), weights(E, 512, 512, group, True, M)
+    check(run(lib, x, off, S, E, w), x, off, E, w)
+
+
+def test_millions_of_rows(lib):
+    """More row blocks than a grid's third dimension counts; the last rows against the oracle, the others with scales of zero."""
+    M, d, f, last = 4194304 + 700, 256, 128, 70
+    off = offsets_of([M - last, last])
+    w = weights(2, d, f, 128, True, 9)
+    for n in ("s_gate", "s_up", "s_down"):
+        w[n][0] = 0.0
+    tail = activations(last, d, 4)
+    c = {k: v.to(DEV) for k, v in w.items()}
+    x = torch.ones(M, d, dtype=torch.bfloat16, device=DEV)
+    x[M - last:] = tail.to(DEV)
+    y = lib.moe_expert_ffn_w4_sliced(x, torch.from_numpy(off).to(DEV), 1, 2, **c)
+    assert not y[: M - last].any().item()
+    check(y[M - last:], tail, offsets_of([last]), 1, {k: v[1:] for k, v in w.items()})
+    # one expert, so that no list of the rows is made: the same rows in the same places
+    y = lib.moe_expert_ffn_w4_sliced(x, torch.tensor([0, M], dtype=torch.int32, device=DEV), 1, 1, **{k: v[1:] for k, v in c.items()})
+    check(y[M - last:], tail, offsets_of([last]), 1, {k: v[1:] for k, v in w.items()})
+    assert torch.equal(y[: M - last], y[:1].expand(M - last, d))

@@ -390,3 +390,30 @@ def test_router_gradients_of_many_experts(lib, kind, E, k, T, renormalise):
             size[t] += 2.0 ** -31 * 2 * s[t] * mean
     # d = p (G - mean): p and the weights to 2^-18 (exponent, sum over E in chains of at most E / 64 and 6 levels), the differences of what is left of it, one rounding at the end
     near(got, ref, 2.0 ** -16 * size + (HALF if kind == "bf16" else 2.0 ** -24) * np.abs(ref) + 1e-30)
+
+
+@pytest.mark.gpu
+def test_more_rows_than_a_launch(lib):
+    """Calls that take several launches: the rows of the later ones get what the same rows get in a small call."""
+    d, rows = 64, 1000
+    T = (1 << 21) + 5
+    x, X = repeated(rows, T, torch.bfloat16, 8, d)
+    z, Z = repeated(rows, T, torch.bfloat16, 9, d)
+    w = torch.linspace(0.5, 1.5, d, device=DEV)
+    tail = T % rows
+    for a, b in zip(lib.moe_block_join(z, x, w, None, w), lib.moe_block_join(Z, X, w, None, w)):
+        assert torch.equal(b[-tail:], a[:tail]) and torch.equal(b[:rows], a)
+    row_of = torch.arange(T, dtype=torch.int32, device=DEV).flip(0).view(T, 1).contiguous()
+    row_of[7] = -1
+    o = lib.moe_combine_topk_sum_backward(Z, X, row_of)
+    want = Z.flip(0)
+    want[T - 8] = 0
+    assert o["d_gate"] is None and torch.equal(o["d_y"], want)
+    T, E = (1 << 24) + 9, 8
+    l, L = repeated(rows, T, torch.float32, 10, E)
+    tail = T % rows
+    small, large = lib.moe_router_topk(l, 2), lib.moe_router_topk(L, 2)
+    assert all(torch.equal(b[-tail:], a[:tail]) for a, b in zip(small, large))
+    dg, DG = repeated(rows, T, torch.float32, 11, 2)
+    for ren in (False, True):
+        assert torch.equal(lib.moe_router_topk_backward(DG, L, large[0], renormalise=ren)[-tail:], lib.moe_router_topk_backward(dg, l, small[0], renormalise=ren)[:tail])
