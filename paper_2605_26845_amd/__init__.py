@@ -579,6 +579,8 @@ def moe_router_topk(logits, topk: int, score: str = "softmax", renormalise: bool
     """logits bf16 or float32 [T][E] -> (ids int32 [T][topk], gates float32 [T][topk]); -inf masks an expert, a slot without expert is (-1, 0)."""
     L, torch, what = load(), _torch, "moe_router_topk"
     T, E = _two(logits, what, "logits")
+    if not 1 <= topk <= E:
+        raise MoeError("%s: topk must be between 1 and the number of experts" % what)
     if ids is None:
         ids = logits.new_empty((T, topk), dtype=torch.int32)
     if gates is None:

@@ -313,7 +313,7 @@ void ffn_w4_stream_kernel(W4Args a, int x_rows) {
 // Two workgroups per compute unit, not three, though smaller tiles leave registers for it: the dispatcher then loads some compute units with three and others with
 // one (54 us above becomes 66).  Measured without a gain: codes or x further ahead; four slices; the sums of x through LDS, a step ahead (117 and 75 us at 8191 rows, 61 and 36 at 203); column
 // tile by column tile, the codes of the next one widened between the products of this one (117 and 71); starting column tiles at different steps; h step by step in
-// memory; a raised priority for the products.  Tiles of 128 x 256 (one wavefront per SIMD, whose sums spill to the matrix cores' half of the registers and are copied for
+// memory; a raised priority for the products; tiles of 128 x 128, which widen half as often (156 and 83 against 64 x 128's 150 and 83).  Tiles of 128 x 256 (one wavefront per SIMD, whose sums spill to the matrix cores' half of the registers and are copied for
 // every multiply-add): 196 and 110.
 template <int PHASE, int TM, int CW, int KS, int NC, int G, bool ZERO>
 __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(CW * KS * 64)

@@ -160,3 +160,13 @@ def test_many_tokens_and_refused_tensors(lib):
                 lambda: lib.moe_router_topk_backward(torch.ones(8, 3, device=DEV), x, ids[:8]), lambda: lib.moe_router_topk_backward(torch.ones(8, 2, device=DEV), x, ids[:8].long())):
         with pytest.raises(lib.MoeError):
             bad()
+
+
+@pytest.mark.gpu
+def test_refused_numbers_of_slots(lib):
+    l = torch.zeros(3, 4, device=DEV)
+    for k in (-1, 0, 5):
+        with pytest.raises(lib.MoeError):
+            lib.moe_router_topk(l, k)
+    ids, gates = lib.moe_router_topk(l, 4)
+    assert ids.tolist() == [[0, 1, 2, 3]] * 3 and gates.tolist() == [[0.25] * 4] * 3
