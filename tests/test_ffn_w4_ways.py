@@ -105,3 +105,20 @@ def test_millions_of_rows(lib):
     y = lib.moe_expert_ffn_w4_sliced(x, torch.tensor([0, M], dtype=torch.int32, device=DEV), 1, 1, **{k: v[1:] for k, v in c.items()})
     check(y[M - last:], tail, offsets_of([last]), 1, {k: v[1:] for k, v in w.items()})
     assert torch.equal(y[: M - last], y[:1].expand(M - last, d))
+
+
+@pytest.mark.parametrize("M", [5, 700])
+def test_most_experts(lib, M):
+    """65536 experts, all that the groups of a schedule allow: rows with the first, the last and some between."""
+    E, d, f, G = 65536, 256, 128, 128
+    some = [0, 1, 32768, 65534, 65535]
+    w = weights(len(some), d, f, G, True, 3)
+    c = {}
+    for n, v in w.items():
+        c[n] = torch.zeros((E,) + tuple(v.shape[1:]), dtype=v.dtype, device=DEV)
+        c[n][torch.tensor(some, device=DEV)] = v.to(DEV)
+    sizes = np.zeros(E, dtype=int)
+    sizes[some] = np.random.default_rng(M).multinomial(M, np.full(len(some), 1.0 / len(some)))
+    x = activations(M, d, M)
+    y = lib.moe_expert_ffn_w4_sliced(x.to(DEV), torch.from_numpy(offsets_of(sizes)).to(DEV), 1, E, **c)
+    check(y, x, offsets_of(sizes[some]), len(some), w)
