@@ -599,8 +599,8 @@ struct TileTimes { int rows, weight_rows, slices; double few, full, shared; };  
 constexpr TileTimes SMALL_TILE = {32, 64, 2, 0.55, 0.82, 0.55}, MIDDLE_TILE = {64, 128, 1, 0.65, 0.90, 0.69}, LARGE_TILE = {64, 256, 1, 0.92, 1.53, 0.97};
 
 struct Phase { int weight_rows, K; };
-double tile_us(const TileTimes& c, const Phase& p, const W4Args& a, int group, bool planned) {
-    const double cus = moe::compute_units(), held = std::max(1, std::min(a.E, a.M)), cols = p.weight_rows / c.weight_rows;
+double tile_us(const TileTimes& c, const Phase& p, const W4Args& a, int group, bool planned, double cus) {
+    const double held = std::max(1, std::min(a.E, a.M)), cols = p.weight_rows / c.weight_rows;
     const double blocks = std::max(held, a.M / (double)c.rows + 0.5 * held), steps = (p.K / W4_STEP + c.slices - 1) / c.slices;
     const double share = blocks * cols / cus, factor = group == 128 ? 1.0 : group == 64 ? 1.06 : 1.24;
     const double alone = a.M / held > c.rows / 2 ? c.full : c.few;
@@ -618,15 +618,15 @@ double stream_us(const Phase& p, const W4Args& a, int group) {
     return 11.3 + passes * (bytes / 4.2e6) * (room || a.M <= 4 ? 1.0 : 1.6) + a.S / 256 * 1.2;
 }
 // the best way of a phase, and its time
-double best_way(const Phase& p, const W4Args& a, int group, bool planned, Way& way) {
+double best_way(const Phase& p, const W4Args& a, int group, bool planned, double cus, Way& way) {
     double least = 1e30;
     auto consider = [&](Way w, double us) { if (us < least) { least = us; way = w; } };
     if (!planned) {
         consider(W4_STREAM, stream_us(p, a, group));
-        consider(W4_SMALL, tile_us(SMALL_TILE, p, a, group, planned));
+        consider(W4_SMALL, tile_us(SMALL_TILE, p, a, group, planned, cus));
     }
-    consider(W4_MIDDLE, tile_us(MIDDLE_TILE, p, a, group, planned));
-    if (group == 128 && (planned || (a.M - 1) / LARGE_TILE.rows < MOST_BLOCKS)) consider(W4_LARGE, tile_us(LARGE_TILE, p, a, group, planned));
+    consider(W4_MIDDLE, tile_us(MIDDLE_TILE, p, a, group, planned, cus));
+    if (group == 128 && (planned || (a.M - 1) / LARGE_TILE.rows < MOST_BLOCKS)) consider(W4_LARGE, tile_us(LARGE_TILE, p, a, group, planned, cus));
     return least;
 }
 
@@ -645,8 +645,9 @@ template <int PHASE, int G, bool ZERO> moe_status launch_way(Way way, const W4Ar
 template <int G, bool ZERO> moe_status both_phases(const W4Args& a, void* plan_at, hipStream_t s) {
     const Phase p1 = {2 * a.f, a.d}, p2 = {a.d, a.f};
     Way w1, w2, v1, v2;
-    const double scanned = best_way(p1, a, G, false, w1) + best_way(p2, a, G, false, w2);
-    const double planned = best_way(p1, a, G, true, v1) + best_way(p2, a, G, true, v2) + 4.4 + a.M * 5e-4;
+    const double cus = moe::compute_units();
+    const double scanned = best_way(p1, a, G, false, cus, w1) + best_way(p2, a, G, false, cus, w2);
+    const double planned = best_way(p1, a, G, true, cus, v1) + best_way(p2, a, G, true, cus, v2) + 4.4 + a.M * 5e-4;
     W4Args p = a;
     if (planned < scanned) {                                               // a launch that lists the rows by expert, for both phases
         moe::RowsPlan plan = {a.offsets, a.S, a.E, a.M, 64, a.row_map, a.row_gate, nullptr, 0, nullptr, nullptr};
