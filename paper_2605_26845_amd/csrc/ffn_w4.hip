@@ -2,10 +2,12 @@
 // point) per group of 32, 64 or 128 inputs:   W[n][k] = (q[n][k] - zero[k / G][n]) * scale[k / G][n].
 //
 // A byte of two codes becomes a pair of bf16 values with a multiplication that copies it to the mantissas of both, a mask, and the exponent: without zero
-// points (16 + q) 2^-12, the four bits above the lowest three of the mantissa; with zero points (48 + q - zero) 2^-12, where q and -zero are added above the lowest two, so
+// points (16 + q) units, the four bits above the lowest three of the mantissa; with zero points (48 + q - zero) units, where q and -zero are added above the lowest two, so
 // that the exponent never changes.  Both exactly.  The matrix cores add products of these with x in fp32 over one group, starting at -24 (16 and the zero point 8)
-// or -48 times 2^-12 times the group's sum of x, which one more product with a constant gives; and the scale multiplies that sum.  So no
-// weight is ever rounded.  (2^-12: the sums of 128 products with the largest finite x stay finite.)
+// or -48 units times the group's sum of x, which one more product with a constant gives; and the scale multiplies that sum.  So no
+// weight is ever rounded.  With a unit of 2^-12 every sum of a group stays finite for the largest finite x, whatever the signs: the codes' part is at most 31 * 128 units of it
+// without zero points and 63 * 64 with them, the start 24 * 128 resp. 48 * 64, and the start with some of the products never more than the start.  Groups of 128 with
+// zero points have twice these terms and a unit of 2^-13.
 #include "lanes.hpp"
 #include "plan.hpp"
 #include "rows.hpp"
@@ -20,9 +22,8 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 
 constexpr int W4_STEP = 128;                    // values of K per step: 16 bytes of codes per lane, 16 weight rows
-constexpr unsigned int MINUS_24 = 0xBBC0BBC0u;  // -24 * 2^-12 twice, in bf16
-constexpr unsigned int MINUS_48 = 0xBC40BC40u;  // -48 * 2^-12 twice
-constexpr float CODE_UNIT = 0x1p12f;
+template <int G, bool ZERO> constexpr float CODE_UNITS = G == 128 && ZERO ? 0x1p13f : 0x1p12f;                      // in one
+template <int G, bool ZERO> constexpr unsigned int START = G == 128 || !ZERO ? 0xBBC0BBC0u : 0xBC40BC40u;      // -24 or -48 units twice, in bf16: -24 * 2^-12 = -48 * 2^-13, or -48 * 2^-12
 
 struct W4Args {
     const __bf16* x; __bf16* h; __bf16* y;      // h: [M][f] in schedule order
@@ -105,8 +106,10 @@ template <int G> __device__ __forceinline__ int k8_of(int i, int g4) {
     return 4 * i + g4;
 }
 
-// What code_values adds: without zero points the exponent of 16 * 2^-12, else 48 * 2^-12 less the zero point
-template <bool ZERO> __device__ __forceinline__ unsigned int code_base(unsigned int zero) { return ZERO ? 0x3C403C40u - (zero & 15u) * 0x00040004u : 0x3B803B80u; }
+// What code_values adds: without zero points the exponent of 16 units, else 48 units less the zero point
+template <int G, bool ZERO> __device__ __forceinline__ unsigned int code_base(unsigned int zero) {
+    return ZERO ? (G == 128 ? 0x3BC03BC0u : 0x3C403C40u) - (zero & 15u) * 0x00040004u : 0x3B803B80u;
+}
 // 8 codes (k, k + 1, .. from the lowest bits) -> 8 values; `mask` is MASK<ZERO> in a register of its own (an instruction holds one constant)
 template <bool ZERO> constexpr unsigned int MASK = ZERO ? 0x003C003Cu : 0x00780078u;
 template <bool ZERO> __device__ __forceinline__ bf16x8 code_values(unsigned int c, unsigned int base, unsigned int mask) {
@@ -238,7 +241,7 @@ void ffn_w4_stream_kernel(W4Args a, int x_rows) {
             }
         };
         auto multiply = [&](Codes& b, const u32x4 (&r)[4]) __attribute__((always_inline)) {
-            const bf16x8 constant = splat(ZERO ? MINUS_48 : MINUS_24);
+            const bf16x8 constant = splat(START<G, ZERO>);
             f32x4 sum[NG];
 #pragma unroll
             for (int i = 0; i < 4; ++i)                                    // what the group's sum starts at
@@ -248,7 +251,7 @@ void ffn_w4_stream_kernel(W4Args a, int x_rows) {
             all_groups<NG>(scale_and_zero<ZERO>(b.s, b.z, row_in), sz);
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
-                const unsigned int base = code_base<ZERO>(sz[gr]);
+                const unsigned int base = code_base<G, ZERO>(sz[gr]);
 #pragma unroll
                 for (int i = gr * PER; i < (gr + 1) * PER; ++i)
                     sum[gr] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r[i]), code_values<ZERO>(b.q[i], base, mask), sum[gr], 0, 0, 0);
@@ -276,8 +279,8 @@ void ffn_w4_stream_kernel(W4Args a, int x_rows) {
                     }
                     const int m = s_row[m16], o = strip * COLS + col;
                     // the hidden activation is rounded to bf16 once, as the operand of the second product
-                    if (PHASE == 1) a.h[(size_t)m * a.f + o] = (__bf16)(silu(CODE_UNIT * s0) * (CODE_UNIT * s1));
-                    else a.y[(size_t)w4_mapped(a, m) * a.d + o] = (__bf16)((a.row_gate ? a.row_gate[m] : 1.0f) * (CODE_UNIT * s0));
+                    if (PHASE == 1) a.h[(size_t)m * a.f + o] = (__bf16)(silu(CODE_UNITS<G, ZERO> * s0) * (CODE_UNITS<G, ZERO> * s1));
+                    else a.y[(size_t)w4_mapped(a, m) * a.d + o] = (__bf16)((a.row_gate ? a.row_gate[m] : 1.0f) * (CODE_UNITS<G, ZERO> * s0));
                 }
             }
             half ^= 1;
@@ -427,7 +430,7 @@ void ffn_w4_tile_kernel(W4Args a) {
                 const int row = t * 16 + r16;
                 return *reinterpret_cast<const bf16x8*>(mem + buffer * X_BYTES + row * 256 + ((k8_of<G>(i, g4) ^ row) & 15) * 16);
             };
-            const bf16x8 constant = splat(ZERO ? MINUS_48 : MINUS_24);
+            const bf16x8 constant = splat(START<G, ZERO>);
             f32x4 acc[NC][T];
 #pragma unroll
             for (int c = 0; c < NC; ++c)
@@ -454,7 +457,7 @@ void ffn_w4_tile_kernel(W4Args a) {
 #pragma unroll
                     for (int c = 0; c < NC; ++c) {
                         scale[c] = __builtin_bit_cast(float, sz[c][gr] & 0xFFFF0000u);
-                        const unsigned int base = code_base<ZERO>(sz[c][gr]);
+                        const unsigned int base = code_base<G, ZERO>(sz[c][gr]);
 #pragma unroll
                         for (int i = 0; i < PER; ++i) w[c][i] = code_values<ZERO>(b.q[c][gr * PER + i], base, mask);
                     }
@@ -528,8 +531,8 @@ void ffn_w4_tile_kernel(W4Args a) {
                     for (int c = 0; c < NH; ++c) {
                         const int o = col0 + c * 16 + r16;
                         // the hidden activation is rounded to bf16 once, as the operand of the second product
-                        if constexpr (PHASE == 1) a.h[(size_t)s_row[r] * a.f + o] = (__bf16)(silu(CODE_UNIT * acc[c][t][v]) * (CODE_UNIT * acc[NH + c][t][v]));
-                        else a.y[(size_t)s_io[r] * a.d + o] = (__bf16)(s_gate[r] * (CODE_UNIT * acc[c][t][v]));
+                        if constexpr (PHASE == 1) a.h[(size_t)s_row[r] * a.f + o] = (__bf16)(silu(CODE_UNITS<G, ZERO> * acc[c][t][v]) * (CODE_UNITS<G, ZERO> * acc[NH + c][t][v]));
+                        else a.y[(size_t)s_io[r] * a.d + o] = (__bf16)(s_gate[r] * (CODE_UNITS<G, ZERO> * acc[c][t][v]));
                     }
                 }
         };
