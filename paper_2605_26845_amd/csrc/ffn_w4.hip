@@ -155,9 +155,9 @@ template <int NG> __device__ __forceinline__ void all_groups(unsigned int v, uns
 // first trip to memory.  From registers alone, a strip per workgroup: 21 and 14; with a workgroup of 16 wavefronts 19 and 13.
 template <int PHASE, int W, bool XLDS, int G, bool ZERO>
 __global__ __attribute__((amdgpu_waves_per_eu(4))) __launch_bounds__(W * 64)
-void ffn_w4_stream_kernel(W4Args a, int x_rows) {
+void ffn_w4_stream_kernel(W4Args a) {
     constexpr int NG = W4_STEP / G, PER = G / 32, D = 4;
-    extern __shared__ __attribute__((aligned(16))) unsigned char s_x[];    // [x_rows][K] bf16, rows 16 bytes further apart (banks)
+    extern __shared__ __attribute__((aligned(16))) unsigned char s_x[];    // [min(M, 16)][K] bf16, rows 16 bytes further apart (banks)
     __shared__ int s_row[16];
     __shared__ int s_scan[W];
     __shared__ f32x4 s_red[2][W][64];
@@ -207,7 +207,7 @@ void ffn_w4_stream_kernel(W4Args a, int x_rows) {
         asked = false;
         const __bf16* const xsrc = PHASE == 1 ? a.x : a.h;
         const int pitch = K * 2 + 16;
-        if constexpr (XLDS) {                                              // (x_rows >= rows: the host counts with M or 16 rows)
+        if constexpr (XLDS) {                                              // (rows is at most M and 16, for which the host asks)
             const int per_row = K / 8, pieces = rows * per_row;
             for (int i0 = tid; i0 < pieces; i0 += W * 64 * 8) {            // 8 pieces of 16 bytes per thread on their way at once
                 u32x4 v[8];
@@ -568,9 +568,18 @@ template <int PHASE, int TM, int CW, int KS, int NC, int G, bool ZERO> moe_statu
 constexpr int STREAM_X_MOST = 124 * 1024;       // LDS for x, beside 16 KiB for the sums
 constexpr int STREAM_W = 8;
 
-template <int PHASE, bool XLDS, int G, bool ZERO> moe_status launch_stream(const W4Args& a, int x_rows, hipStream_t s) {
-    const int K = PHASE == 1 ? a.d : a.f, strips = PHASE == 1 ? a.f / 8 : a.d / 16;
-    const int lds = XLDS ? x_rows * (K * 2 + 16) : 0;
+// LDS for x in a streaming launch, 0 where it has no room
+int stream_lds(const W4Args& a, int K) {
+    const int lds = std::min(a.M, 16) * (K * 2 + 16);
+    return lds <= STREAM_X_MOST ? lds : 0;
+}
+// two workgroups per compute unit, as far as their LDS allows, for the experts that can hold rows
+dim3 stream_grid(const W4Args& a, int strips, int lds) {
+    const int per_cu = lds > 60 * 1024 ? 1 : 2, held = std::max(1, std::min(a.E, a.M));
+    return dim3(std::min(strips, std::max(1, moe::compute_units() * per_cu / held)), a.E, std::min((a.M - 1) / 16 + 1, 8));
+}
+
+template <int PHASE, bool XLDS, int G, bool ZERO> moe_status launch_stream(const W4Args& a, int lds, hipStream_t s) {
     auto kern = ffn_w4_stream_kernel<PHASE, STREAM_W, XLDS, G, ZERO>;
     if (XLDS) {
         static moe::DeviceOnce attr;
@@ -581,17 +590,17 @@ template <int PHASE, bool XLDS, int G, bool ZERO> moe_status launch_stream(const
             attr.mark(dev);
         }
     }
-    // two workgroups per compute unit, as far as their LDS allows, for the experts that can hold rows
-    const int per_cu = lds > 60 * 1024 ? 1 : 2, held = std::max(1, std::min(a.E, a.M));
-    const int grid = std::min(strips, std::max(1, moe::compute_units() * per_cu / held));
     moe::LaunchScope k(PHASE == 1 ? "ffn_w4_stream1_kernel" : "ffn_w4_stream2_kernel", s);
-    hipLaunchKernelGGL(kern, dim3(grid, a.E, std::min((a.M - 1) / 16 + 1, 8)), dim3(STREAM_W * 64), lds, s, a, x_rows);
+    hipLaunchKernelGGL(kern, stream_grid(a, PHASE == 1 ? a.f / 8 : a.d / 16, lds), dim3(STREAM_W * 64), lds, s, a);
     return k.done();
 }
 
 // ---- which kernel a phase takes, by estimates (us).  M bounds the rows; how they spread over the experts is not known here.
-// Fitted to 167 shapes (E 1 .. 32, d 256 .. 7168, f 512 .. 14336, 1 .. 8191 rows, groups of 32, 64 and 128), every phase timed in every way; the choice is within
-// 8 % of the best of them but for 5 shapes (32 experts of 1024 x 512 with 256 rows: 33 against 28).  Streaming / tiles of 32 x 64 / 64 x 128 / 64 x 256, us, groups of
+// Fitted to 168 shapes (E 1 .. 32, d 256 .. 7168, f 512 .. 14336, 1 .. 8191 rows, groups of 32, 64 and 128), every phase timed in every way; the choice takes 1.4 % longer than
+// the best of them in the mean, and over 8 % longer in 8 shapes (one expert of 4096 x 4096 with 4 rows: 33 us against 26).  What a streaming workgroup costs that finds no rows was
+// measured on 196 more (E 1 .. 2048, 1 .. 600 rows on experts of uneven popularity): 0.0031 us, so that one row on 128 experts of 2048 x 768 streams in 49 + 62 us and takes 13 + 15 in
+// tiles of 32 x 64.  There the choice is 15 % behind in the mean and 2.4 times at most (one row on 2048 experts of 256 x 128: 31 against 13, of which the list 18; one on 128 of 7168 x 512: 56
+// against 29; idle workgroups of the tiles cost half of what they are taken for with that many experts).  Streaming / tiles of 32 x 64 / 64 x 128 / 64 x 256, us, groups of
 // 128, phase 1 + phase 2 (the tiles of 64 rows with a list of the rows, whose own launch takes 5 and with more rows up to 10):
 //   E 1, d 4096, f 14336:   1 row 21+14  20+36  26+73  34+115,  12 rows 23+20  19+36  27+74  35+115,  96 rows 218+108  62+45  46+98  53+174,  400 rows -  227+107  150+101  132+175
 //   E 4, d 7168, f 2048:    4 rows 21+14  21+11  38+14  57+18,  24 rows 35+18  24+12  40+15  58+19,   200 rows 143+55  41+29  55+25  89+29,   1000 rows -  148+104  111+51  120+43
@@ -617,8 +626,10 @@ double tile_us(const TileTimes& c, const Phase& p, const W4Args& a, int group, b
 double stream_us(const Phase& p, const W4Args& a, int group) {
     const double held = std::max(1, std::min(a.E, a.M)), passes = std::ceil(std::min<double>(a.M, 3.0 * a.M / held) / 16);      // over the most popular expert's weights
     const double bytes = held * p.weight_rows * (p.K / 2.0) * (1.0 + 4.0 / group);
-    const bool room = std::min(a.M, 16) * (p.K * 2 + 16) <= STREAM_X_MOST;
-    return 11.3 + passes * (bytes / 4.2e6) * (room || a.M <= 4 ? 1.0 : 1.6) + a.S / 256 * 1.2;
+    const int lds = stream_lds(a, p.K);
+    const dim3 grid = stream_grid(a, p.weight_rows / 16, lds);
+    const double idle = std::max(0.0, grid.x * ((double)grid.y * grid.z - held * std::min<double>(grid.z, passes)));      // workgroups that find no rows
+    return 11.3 + passes * (bytes / 4.2e6) * (lds > 0 || a.M <= 4 ? 1.0 : 1.6) + a.S / 256 * 1.2 + idle * 0.0031;
 }
 // the best way of a phase, and its time
 double best_way(const Phase& p, const W4Args& a, int group, bool planned, double cus, Way& way) {
@@ -636,8 +647,8 @@ double best_way(const Phase& p, const W4Args& a, int group, bool planned, double
 template <int PHASE, int G, bool ZERO> moe_status launch_way(Way way, const W4Args& a, hipStream_t s) {
     switch (way) {
         case W4_STREAM: {
-            const int rows = std::min(a.M, 16), K = PHASE == 1 ? a.d : a.f;
-            return rows * (K * 2 + 16) <= STREAM_X_MOST ? launch_stream<PHASE, true, G, ZERO>(a, rows, s) : launch_stream<PHASE, false, G, ZERO>(a, rows, s);
+            const int lds = stream_lds(a, PHASE == 1 ? a.d : a.f);
+            return lds > 0 ? launch_stream<PHASE, true, G, ZERO>(a, lds, s) : launch_stream<PHASE, false, G, ZERO>(a, 0, s);
         }
         case W4_SMALL: return launch_tile<PHASE, 2, 2, 2, 2, G, ZERO>(a, s);
         case W4_LARGE:
