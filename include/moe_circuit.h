@@ -369,7 +369,7 @@ moe_status moe_router_topk_backward(const float* d_gates, const void* logits, in
  *            out[t]  = scale * stream[t] + gate[t] * u   (without gate: gate = 1)
  *            next[t] = out[t] / rms(out[t]) * next_weight              (the input of the next block; without next_weight: not made)
  * Arithmetic in fp32, next from out before out is rounded; a row whose sum of squares passes the range of fp32 counts as
- * infinitely long (normalised to zeros).
+ * infinitely long (normalised to zeros, and in the backward passes without a gradient through its norm).
  *   x, stream, out (of join)  [T][d], bf16 or float (stream_type: MOE_T_BF16 / MOE_T_F32): the residual stream
  *   z, next, out (of norm)    bf16 [T][d]            weights  float [d]            gate  float [T]
  *   out may be the stream itself, and next may be z (the same pointer): a row is read before it is written.

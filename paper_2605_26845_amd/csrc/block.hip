@@ -214,7 +214,8 @@ void block_backward_kernel(BackwardArgs a) {
         }
         moe::workgroup_sums<NT>(sum, s_sum3, half3);
         const float r2 = inverse_rms(sum[0], a.d, a.eps), r1 = JOIN && a.w1 ? inverse_rms(sum[2], a.d, a.eps) : 1.0f;
-        const float back2 = sum[1] * by_d * r2 * r2;
+        // (an infinitely long row, r = 0, has no gradient through its norm, whatever its product with the gradient came to: that may have passed fp32 as well)
+        const float back2 = r2 == 0.0f ? 0.0f : sum[1] * by_d * r2 * r2;
         float D[NV][8], q[1] = {0.f};
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
@@ -253,6 +254,7 @@ void block_backward_kernel(BackwardArgs a) {
         }
         if constexpr (JOIN) {
             if (a.w1 || a.d_gate) moe::workgroup_sums<NT>(q, s_sum1, half1);
+            if (r1 == 0.0f) q[0] = 0.0f;
             if (a.d_gate && tid == 0) a.d_gate[row] = q[0] * r1;
             const float back1 = a.w1 ? q[0] * by_d * r1 * r1 : 0.0f, rg1 = r1 * g;
 #pragma unroll
