@@ -365,7 +365,10 @@ template <bool F32, bool JOIN> moe_status backward_of(const BackwardArgs& a, flo
     if (a.d <= 2048) return backward<256, 1, F32, JOIN>(a, d_w1, d_w2, work, s);
     if (a.d <= 2736) return backward<256, 2, F32, JOIN>(a, d_w1, d_w2, work, s);
     if (a.d <= 4096) return backward<512, 1, F32, JOIN>(a, d_w1, d_w2, work, s);
-    if (a.d <= 8192) return F32 || a.T <= 1024 ? backward<1024, 1, F32, JOIN>(a, d_w1, d_w2, work, s) : backward<512, 2, F32, JOIN>(a, d_w1, d_w2, work, s);
+    if constexpr (!F32) {
+        if (a.d <= 8192 && a.T > 1024) return backward<512, 2, F32, JOIN>(a, d_w1, d_w2, work, s);
+    }
+    if (a.d <= 8192) return backward<1024, 1, F32, JOIN>(a, d_w1, d_w2, work, s);
     return backward<1024, 2, F32, JOIN>(a, d_w1, d_w2, work, s);
 }
 
