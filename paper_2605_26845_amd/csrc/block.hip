@@ -5,8 +5,8 @@
 //
 // All of it is one pass over the rows: a row stays in registers between the two sums over its columns, so z and the stream are read once and
 // out and next written once.  HBM bound; a thread owns 8 consecutive columns per step (16 bytes of bf16).  A row of up to 1024 columns belongs to
-// one wavefront (no barriers, four rows per workgroup), a longer one to a workgroup.  16381 rows of 7168 in bf16: 167 us, 5.6 TB/s (with 256 threads and four steps a row 184); one row of 4096:
-// 3.1 us, a launch and two trips to memory.
+// one wavefront (no barriers, four rows per workgroup), a longer one to a workgroup.  16381 rows of 7168 in bf16: 168 us, 5.6 TB/s (with 256 threads and four steps a row 184), the
+// first dozens of passes after a pause 183; 4096 rows of 16384, two steps of 1024 threads: 101 us, 5.3 TB/s; one row of 4096: 2.6 us, a launch and two trips to memory.
 #include "lanes.hpp"
 #include <algorithm>
 
@@ -162,6 +162,8 @@ struct BackwardArgs {
 // Three sums over the columns of a row meet in one reduction (out^2, d_next w2 out, z^2), the fourth (D w1 z) in a second one.
 // The sums over the tokens stay in registers while a workgroup walks its rows; four wavefronts per SIMD (without the bound on registers a workgroup of 256 had two or three: 137
 // against 127 us).  8192 rows of 4096 with a float32 stream: 119 us, 5.1 TB/s, and 5 for the sums over the workgroups.
+// Above 8192 columns two steps of 1024 threads do not fit the 128 registers that such a workgroup leaves each: the join's kernel spills 19 of them with a bf16 stream and 58 with float32
+// (4096 rows of 16384: 202 us, 3.9 TB/s, and 326 us, 3.6 TB/s; the norm's does not spill: 94 and 138 us). Two steps of a wavefront with a float32 stream spill 9.
 template <int NT, int NV, bool F32, bool JOIN>
 __global__ __attribute__((amdgpu_waves_per_eu(4))) __launch_bounds__(NT == 64 ? 256 : NT)
 void block_backward_kernel(BackwardArgs a) {

@@ -152,7 +152,7 @@ template <int NG> __device__ __forceinline__ void all_groups(unsigned int v, uns
 // fragments of the matrix instruction, D - 1 steps ahead and across the strips.  The W partial sums of a strip meet in LDS and are added in a fixed
 // order while the next strip's codes arrive.  x lies in LDS if it has room there (XLDS); otherwise its fragments are fetched a step ahead.
 // One row of one expert, d 4096, f 14336, groups of 128 (88 MB of codes): phases 18 and 12 us, 3.3 and 2.4 TB/s, of which about 5 us each are the launch and the
-// first trip to memory.  From registers alone, a strip per workgroup: 21 and 14; with a workgroup of 16 wavefronts 19 and 13.
+// first trip to memory (the call takes tiles of 32 x 64 for the first, 17 us).  With zero points and groups of 32 or 64 up to 5 registers are spilled.  From registers alone, a strip per workgroup: 21 and 14; with a workgroup of 16 wavefronts 19 and 13.
 template <int PHASE, int W, bool XLDS, int G, bool ZERO>
 __global__ __attribute__((amdgpu_waves_per_eu(4))) __launch_bounds__(W * 64)
 void ffn_w4_stream_kernel(W4Args a) {
@@ -278,7 +278,8 @@ void ffn_w4_stream_kernel(W4Args a) {
                         for (int w = 0; w < W; ++w) s1 += red[w * 256 + at + 32];
                     }
                     const int m = s_row[m16], o = strip * COLS + col;
-                    // the hidden activation is rounded to bf16 once, as the operand of the second product
+                    // The hidden activation is rounded to bf16 once, as the operand of the second product, as in the library's other FFN calls: the results' error (2-norm, of their size)
+                    // is 2.3e-3 with it and would be 1.7e-3 from y's own rounding; silu's reciprocal and exponential are the hardware's, a step each.
                     if (PHASE == 1) a.h[(size_t)m * a.f + o] = (__bf16)(silu(CODE_UNITS<G, ZERO> * s0) * (CODE_UNITS<G, ZERO> * s1));
                     else a.y[(size_t)w4_mapped(a, m) * a.d + o] = (__bf16)((a.row_gate ? a.row_gate[m] : 1.0f) * (CODE_UNITS<G, ZERO> * s0));
                 }
@@ -336,7 +337,7 @@ void ffn_w4_tile_kernel(W4Args a) {
     unsigned int mask = MASK<ZERO>;
     asm("" : "+v"(mask));
     int e, rows, col_tile;
-    for (int z = blockIdx.z;; z += gridDim.z) {                            // (a workgroup that follows a list has one block; so have the largest tiles, whose registers a loop would spill)
+    for (int z = blockIdx.z;; z += gridDim.z) {                            // (a workgroup that follows a list has one block; so have the largest tiles, of whose registers a loop would spill more than the 4, with zero points 11, that are spilled)
         if (a.blocks) {
             // neighbouring workgroups of a die (every eighth one) take the column tiles of one row block, whose rows then stay in its L2; with few row blocks
             // the dies share them
@@ -530,7 +531,7 @@ void ffn_w4_tile_kernel(W4Args a) {
 #pragma unroll
                     for (int c = 0; c < NH; ++c) {
                         const int o = col0 + c * 16 + r16;
-                        // the hidden activation is rounded to bf16 once, as the operand of the second product
+                        // (the hidden activation's rounding: see the streaming kernel)
                         if constexpr (PHASE == 1) a.h[(size_t)s_row[r] * a.f + o] = (__bf16)(silu(CODE_UNITS<G, ZERO> * acc[c][t][v]) * (CODE_UNITS<G, ZERO> * acc[NH + c][t][v]));
                         else a.y[(size_t)s_io[r] * a.d + o] = (__bf16)(s_gate[r] * (CODE_UNITS<G, ZERO> * acc[c][t][v]));
                     }

@@ -1,10 +1,11 @@
 // moe_router_topk and its backward pass: the router of a MoE block (Section 2.1: each token is sent to its top-k experts), from logits to
 // the expert ids that the histogram counts and the weights that the combine takes.
 //
-// LANES neighbouring lanes own a token and VPL neighbouring experts each: the logits are read once with wide loads.  Every lane sorts
+// LANES neighbouring lanes own a token and VPL neighbouring experts each: the logits are read once, 16 bytes at a time where a lane's neighbours are that many and rows start on 16
+// bytes (4 float32 or 8 bf16 experts per lane and more), else one by one: with up to 16 experts, and in bf16 up to 64, and 129 to 256 for few tokens.  Every lane sorts
 // its experts by (logit, lower index first); the largest head of all lanes is taken topk times, and the lane that held it moves its list up.
 // (More than 4 experts per lane are looked through each time instead: sorting them is a quadratic number of exchanges.)
-// Bound by the vector instructions of the choice, with few tokens by its chain: 32771 tokens of 64 experts, top-2, in bf16 7.1 us, 64 tokens of 256, top-8, 4.8 us.
+// Bound by the vector instructions of the choice, with few tokens by its chain: 32771 tokens of 64 experts, top-2, in bf16 6.8 us, 64 tokens of 256, top-8, 4.2 us.
 // Neither the order of the lanes nor any atomic decides a tie: equal logits go to the lower index.
 #include "lanes.hpp"
 #include <algorithm>
@@ -195,7 +196,7 @@ void router_topk_kernel(RouterArgs a) {
 //   renormalised (w_j sum to one over the slots)      d_l[id_j] += w_j (1 - sigmoid(l_j) for sigmoid scores, else 1) (G_j - sum_k G_k w_k)
 //   sigmoid                 d_l[id_j] += G_j s_j (1 - s_j)
 // What a slot gives its expert meets the expert's lane in LDS, a row of E floats per token.  Bound by the vector instructions of the exponentials: each is taken once
-// (16384 tokens of 256 experts, top-8: 10.5 us, 3.2 TB/s; with a second one per logit, a wavefront per token and every lane asking every slot 16.5 us).
+// (16384 tokens of 256 experts, top-8: 10.8 us, 3.1 TB/s; with a second one per logit, a wavefront per token and every lane asking every slot 16.5 us).
 template <bool F32, int LANES, int VPL, bool WIDE>
 __global__ __launch_bounds__(ROUTER_THREADS)
 void router_backward_kernel(RouterArgs a) {
@@ -340,8 +341,10 @@ template <bool F32, int LANES, int VPL> moe_status launch_topk(RouterArgs a, boo
     return k.done();
 }
 template <bool F32> moe_status topk_of(const RouterArgs& a, bool wide, hipStream_t s) {
-    // 16 experts per lane cost the fewest instructions (32768 tokens of 128 experts, top-6: 8 lanes 12.6 us, 16 lanes of 8 experts 20; 16384 of 256, top-8: 16 lanes 14.4, 32 of 8
-    // 26, 64 of 4 21; 8192 of 512: 32 lanes 14, 64 of 8 25), four sorted ones per lane the shortest chain (64 tokens of 256: 4.8 against 7.1, level at some 4000 tokens)
+    // (Times with the events around the launch, about 0.6 us more than the kernel's.)  16 experts per lane cost the fewest instructions (32768 tokens of 128 experts, top-6: 8 lanes 12.6 us, 16 lanes of 8 experts 20; 16384 of 256, top-8: 16 lanes 14.4, 32 of 8
+    // 26, 64 of 4 21; 8192 of 512: 32 lanes 14, 64 of 8 25), four sorted ones per lane the shortest chain (64 tokens of 256: 4.8 against 7.1, level at some 4000 tokens).
+    // Up to 64 experts the two are near each other and the chain counts: 32768 tokens of 64, top-2, 16 lanes of 4 7.4 us, 8 of 8 8.5, 4 of 16 7.8, top-8 8.9, 8.5 and 9.0; 4096 tokens, top-8,
+    // 6.9, 8.3 and 7.9
     if (a.E <= 16) return launch_topk<F32, 16, 1>(a, wide, s);
     if (a.E <= 64) return launch_topk<F32, 16, 4>(a, wide, s);
     if (a.E <= 128) return launch_topk<F32, 8, 16>(a, wide, s);
