@@ -575,9 +575,9 @@ int stream_lds(const W4Args& a, int K) {
     return lds <= STREAM_X_MOST ? lds : 0;
 }
 // two workgroups per compute unit, as far as their LDS allows, for the experts that can hold rows
-dim3 stream_grid(const W4Args& a, int strips, int lds) {
+dim3 stream_grid(const W4Args& a, int strips, int lds, int cus) {
     const int per_cu = lds > 60 * 1024 ? 1 : 2, held = std::max(1, std::min(a.E, a.M));
-    return dim3(std::min(strips, std::max(1, moe::compute_units() * per_cu / held)), a.E, std::min((a.M - 1) / 16 + 1, 8));
+    return dim3(std::min(strips, std::max(1, cus * per_cu / held)), a.E, std::min((a.M - 1) / 16 + 1, 8));
 }
 
 template <int PHASE, bool XLDS, int G, bool ZERO> moe_status launch_stream(const W4Args& a, int lds, hipStream_t s) {
@@ -592,7 +592,7 @@ template <int PHASE, bool XLDS, int G, bool ZERO> moe_status launch_stream(const
         }
     }
     moe::LaunchScope k(PHASE == 1 ? "ffn_w4_stream1_kernel" : "ffn_w4_stream2_kernel", s);
-    hipLaunchKernelGGL(kern, stream_grid(a, PHASE == 1 ? a.f / 8 : a.d / 16, lds), dim3(STREAM_W * 64), lds, s, a);
+    hipLaunchKernelGGL(kern, stream_grid(a, PHASE == 1 ? a.f / 8 : a.d / 16, lds, moe::compute_units()), dim3(STREAM_W * 64), lds, s, a);
     return k.done();
 }
 
@@ -624,20 +624,20 @@ double tile_us(const TileTimes& c, const Phase& p, const W4Args& a, int group, b
     }
     return us;
 }
-double stream_us(const Phase& p, const W4Args& a, int group) {
+double stream_us(const Phase& p, const W4Args& a, int group, int cus) {
     const double held = std::max(1, std::min(a.E, a.M)), passes = std::ceil(std::min<double>(a.M, 3.0 * a.M / held) / 16);      // over the most popular expert's weights
     const double bytes = held * p.weight_rows * (p.K / 2.0) * (1.0 + 4.0 / group);
     const int lds = stream_lds(a, p.K);
-    const dim3 grid = stream_grid(a, p.weight_rows / 16, lds);
+    const dim3 grid = stream_grid(a, p.weight_rows / 16, lds, cus);
     const double idle = std::max(0.0, grid.x * ((double)grid.y * grid.z - held * std::min<double>(grid.z, passes)));      // workgroups that find no rows
     return 11.3 + passes * (bytes / 4.2e6) * (lds > 0 || a.M <= 4 ? 1.0 : 1.6) + a.S / 256 * 1.2 + idle * 0.0031;
 }
 // the best way of a phase, and its time
-double best_way(const Phase& p, const W4Args& a, int group, bool planned, double cus, Way& way) {
+double best_way(const Phase& p, const W4Args& a, int group, bool planned, int cus, Way& way) {
     double least = 1e30;
     auto consider = [&](Way w, double us) { if (us < least) { least = us; way = w; } };
     if (!planned) {
-        consider(W4_STREAM, stream_us(p, a, group));
+        consider(W4_STREAM, stream_us(p, a, group, cus));
         consider(W4_SMALL, tile_us(SMALL_TILE, p, a, group, planned, cus));
     }
     consider(W4_MIDDLE, tile_us(MIDDLE_TILE, p, a, group, planned, cus));
@@ -660,7 +660,7 @@ template <int PHASE, int G, bool ZERO> moe_status launch_way(Way way, const W4Ar
 template <int G, bool ZERO> moe_status both_phases(const W4Args& a, void* plan_at, hipStream_t s) {
     const Phase p1 = {2 * a.f, a.d}, p2 = {a.d, a.f};
     Way w1, w2, v1, v2;
-    const double cus = moe::compute_units();
+    const int cus = moe::compute_units();
     const double scanned = best_way(p1, a, G, false, cus, w1) + best_way(p2, a, G, false, cus, w2);
     const double planned = best_way(p1, a, G, true, cus, v1) + best_way(p2, a, G, true, cus, v2) + 4.4 + a.M * 5e-4;
     W4Args p = a;
